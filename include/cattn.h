@@ -301,6 +301,185 @@ cattn_status cattn_sce_fwd(const float* logits, const int* targets, float* lse,
 cattn_status cattn_sce_bwd(const float* logits, const int* targets, const float* lse,
                            float scale, float* dlogits, int rows, int V, void* stream);
 
+/*
+ * Decoder-block operators: root-mean-square norm, rotary positions and
+ * sliding-window attention, in training and for single tokens.  They follow the
+ * conventions above (device pointers, asynchronous on `stream`, no allocation,
+ * no state, deterministic, argument errors before anything is enqueued) with
+ * these differences.
+ *
+ * Query and key/value heads may be grouped: Hq a multiple of Hkv, and query
+ * head h reads key/value head h / (Hq / Hkv).
+ *
+ * Tensors of heads may be strided views, for instance of one projection's
+ * output: where an entry point takes `strides`, it is NULL (every tensor is
+ * contiguous in `layout`) or the element strides of batch, head and row, three
+ * per tensor, in the order of the tensors in the argument list.  A row's D
+ * columns are consecutive.  Strides are not negative; the stride of a dimension
+ * of size 1 is not looked at; an output's elements are distinct.  Outputs must
+ * not share elements with inputs or with each other (interleaved views of one
+ * allocation do not); what the entry points cannot tell apart they refuse.
+ *
+ * RMSNorm of the rows of x [rows, C], with the residual stream's addition:
+ *     h = x + residual        (residual NULL: h = x, and `h` must be NULL)
+ *     rstd = 1 / sqrt(mean_c(h^2) + eps)
+ *     y = h * rstd * gamma
+ *   x, residual, y, h: [rows, C] `dtype`; gamma: float [C]; rstd: out, float
+ *   [rows].  Sums are float; y comes from the unrounded h, and is rounded once,
+ *   as is the h that is stored.
+ *   Supported: C a multiple of 8 and at most 16384, rows at most 2^30; eps
+ *   finite and >= 0.  Tensors 16-byte aligned (rstd: 4).
+ */
+cattn_status cattn_rmsnorm_fwd(const void* x, const void* residual, const float* gamma, void* y, void* h, float* rstd,
+                               int rows, int C, float eps, int dtype, void* stream);
+
+/* The same with y in 8 bits: q [rows, C] are e4m3 (OCP: finite to +-448) codes
+ * and scale [rows, ceil(C / group)] their float scales, one per `group`
+ * consecutive columns of a row (the last group may be shorter; group 0: one
+ * per row):
+ *     scale = max(max|y| / 448, 2^-126),  q = e4m3(y / scale)   (to nearest even)
+ * A NaN of y stays one in q.  group: 0, or a power of two from 8 to 512
+ * (CATTN_ERR_INVALID_ARG otherwise).  q is 16-byte aligned, scale 4-byte. */
+cattn_status cattn_rmsnorm_fwd_q8(const void* x, const void* residual, const float* gamma, unsigned char* q,
+                                  float* scale, void* h, float* rstd, int rows, int C, int group, float eps, int dtype,
+                                  void* stream);
+
+/* RMSNorm backward for upstream dy, with the forward's h (x where there was no
+ * residual) and rstd, xhat = h * rstd, g = dy * gamma:
+ *     dx = rstd * (g - xhat * mean_c(g * xhat)) + dh     (`dtype`)
+ *     dgamma = sum_r dy * xhat                           (float [C])
+ * dh, or NULL: the gradient that reaches h beside the norm; dx is then the
+ * gradient of both x and residual.  workspace: at least
+ * cattn_rmsnorm_bwd_workspace_bytes(rows, C) bytes, 16-byte aligned (partial
+ * rows of dgamma). */
+cattn_status cattn_rmsnorm_bwd(const void* h, const float* gamma, const float* rstd, const void* dy, const void* dh,
+                               void* dx, float* dgamma, float* workspace, int rows, int C, int dtype, void* stream);
+size_t cattn_rmsnorm_bwd_workspace_bytes(int rows, int C);
+
+/* Scaling of rotary frequencies for contexts longer than the trained one. */
+typedef enum {
+  CATTN_ROPE_NONE = 0,    /* f_i = base^(-2i / rot) */
+  CATTN_ROPE_LINEAR = 1,  /* f_i / factor: positions interpolated */
+  CATTN_ROPE_NTK = 2,     /* base * factor^(rot / (rot - 2)) in place of base (rot > 2) */
+  CATTN_ROPE_RAMP = 3     /* by the turns t_i = context f_i / 2 pi a pair makes in the trained context:
+                             f_i where t_i >= high, f_i / factor where t_i <= low, between them
+                             linear in t_i */
+} cattn_rope_scaling;
+
+/* The rot / 2 frequencies, radians per position, into HOST memory `freqs`.
+ * rot even and > 0, base > 0, factor >= 1, context > 0 and low < high where they
+ * are used, all finite (CATTN_ERR_INVALID_ARG otherwise). */
+cattn_status cattn_rope_frequencies(double* freqs, int rot, double base, int scaling, double factor, double context,
+                                    double low, double high);
+
+/*
+ * Rotary positions of queries and keys: with angle p * freqs[i], p the token's
+ * position, the pair (a, b) of columns becomes
+ *     (a cos - b sin, b cos + a sin) * amplitude
+ * Pairs are columns (i, i + rot / 2) for interleaved == 0, (2i, 2i + 1)
+ * otherwise, i < rot / 2; columns from rot on are copied.  inverse != 0 turns by
+ * the negative angle: the backward (dq, dk in place of q, k).  Angles are formed
+ * in double.
+ *
+ *   q, q_out: [B, Hq, S, D] and k, k_out: [B, Hkv, S, D] `dtype` in `layout`'s
+ *             order, or strided (order: q, k, q_out, k_out).  k and k_out may be
+ *             NULL with Hkv = 0.  q_out may be q, and k_out k (same address and
+ *             strides): rotated in place.
+ *   positions: int32 [B, S] (batched != 0) or [S], or NULL: 0 .. S - 1
+ *   freqs:    DEVICE double [rot / 2]
+ * Supported: D even, 2 .. 512; rot even, 2 .. D; B * S < 2^31.  Any strides and
+ * element-aligned addresses; 16-byte ones with rot / 2 (interleaved: rot) and
+ * D - rot multiples of 16 bytes are the fast path.
+ */
+cattn_status cattn_rope(const void* q, const void* k, void* q_out, void* k_out, const int* positions,
+                        const double* freqs, int B, int S, int Hq, int Hkv, int D, int rot, int batched,
+                        const long long* strides, int layout, int interleaved, int inverse, float amplitude, int dtype,
+                        void* stream);
+
+/*
+ * Rotary positions of the new tokens of a batch, and their keys and values into
+ * a cache, in one pass.
+ *
+ *   q, q_out, k, k_out: as for cattn_rope; v [B, Hkv, S, D]
+ *   k_cache, v_cache: in/out, [B, Hkv, cap, D] (strides order: q, k, v, q_out,
+ *             k_out, k_cache, v_cache)
+ *   lens:     int32 [B], the tokens of each sequence after this call
+ *   counts:   int32 [B] or NULL: how many of the S tokens are the sequence's
+ *             (the first counts[b], clamped to 0 .. S; NULL: all).  Token i of
+ *             sequence b is at position lens[b] - counts[b] + i.
+ * A token past counts[b], or at a negative position, is none: its q_out and
+ * k_out are 0 and nothing is stored.  The rotated key and the value at position
+ * p go to
+ *   slot p where rolling == 0 (dropped where p >= cap; window, sinks unused);
+ *   where rolling != 0, slot p if p < sinks, else sinks + (p - sinks) % window,
+ *   if p is among the sequence's last `window` positions: such a cache holds
+ *   what a window with sinks can see (window >= 1, sinks >= 0, sinks + window <= cap).
+ * Other slots are left as they are.
+ */
+cattn_status cattn_rope_append(const void* q, const void* k, const void* v, void* q_out, void* k_out, void* k_cache,
+                               void* v_cache, const int* lens, const int* counts, const double* freqs, int B, int S,
+                               int Hq, int Hkv, int D, int rot, int cap, int window, int sinks, int rolling,
+                               const long long* strides, int layout, int interleaved, float amplitude, int dtype,
+                               void* stream);
+
+/*
+ * Sliding-window attention with sinks: causal attention in which query i sees
+ * key j iff
+ *     j <= i  and  (i - j < window  or  j < sinks)
+ * (window counts the query itself; window >= S is plain causal attention).
+ * Forward and backward compute cattn_attn_fwd's and cattn_attn_bwd's formulas
+ * over those pairs; dK and dV sum over the query heads of a group.
+ *
+ *   q, o, dout, dq: [B, Hq, S, D]; k, v, dk, dv: [B, Hkv, S, D] `dtype`, in
+ *             `layout`'s order or strided (order: q, k, v, o of the forward; q,
+ *             k, v, o, dout, dq, dk, dv of the backward)
+ *   lse:      float [B, Hq, S], contiguous
+ *   lens:     int32 [B] or NULL: sequence b has lens[b] tokens (clamped to 0 ..
+ *             S), rows from there on are padding.  They are not read, and what
+ *             they hold does not matter; their o, dq, dk and dv are 0, their lse
+ *             -infinity.  (A value of a token itself that is not finite may reach
+ *             rows that do not see it but share its 32-row tile.)
+ *   workspace: at least cattn_swa_bwd_workspace_bytes(...) bytes, 16-byte aligned
+ * Supported: D in {64, 128}; S <= 2^26; B * Hq * ceil(S / 32) < 2^31; window >=
+ * 1, sinks >= 0; scale in [1e-20, 1e6]; tensors 16-byte aligned, with strides of
+ * whole 16 bytes and row strides below 2^23 elements.
+ */
+cattn_status cattn_swa_fwd(const void* q, const void* k, const void* v, void* o, float* lse, const int* lens, int B,
+                           int Hq, int Hkv, int S, int D, int window, int sinks, float scale,
+                           const long long* strides, int layout, int dtype, void* stream);
+cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                           const float* lse, const int* lens, void* dq, void* dk, void* dv, float* workspace, int B,
+                           int Hq, int Hkv, int S, int D, int window, int sinks, float scale,
+                           const long long* strides, int layout, int dtype, void* stream);
+size_t cattn_swa_bwd_workspace_bytes(int B, int Hq, int Hkv, int S, int D, int window, int sinks);
+
+/*
+ * Sliding-window attention with sinks for single tokens: one query per
+ * sequence, the newest of its lens[b] tokens, over a cache that holds them (its
+ * own key and value included), as cattn_rope_append leaves it.
+ *
+ *   q, o:     [B, Hq, D] (strides: batch, head, and a third that is not looked at)
+ *   k_cache, v_cache: [B, Hkv, cap, D] (strides order: q, k_cache, v_cache, o).
+ *             Only visible slots are read: what others hold does not matter.
+ *   lens:     int32 [B], tokens of each sequence; 0 (or less): an empty row, o is
+ *             0 and lse -infinity
+ *   rolling == 0: slot j holds position j; lens[b] is at most cap (a larger one
+ *             is taken as cap).  The query sees the last `window` positions and
+ *             those below sinks.
+ *   rolling != 0: the cache is cattn_rope_append's for the same window and sinks
+ *             (sinks + window <= cap); the query sees the first min(lens[b],
+ *             sinks + window) slots, all that it holds.
+ *   lse:      out, float [B, Hq]
+ *   workspace: at least cattn_swa_decode_workspace_bytes(...) bytes, 16-byte
+ *             aligned; may be NULL where that is 0
+ * Supported: as for cattn_swa_fwd, with cap <= 2^26 in place of S.
+ */
+cattn_status cattn_swa_decode(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
+                              const int* lens, float* workspace, int B, int Hq, int Hkv, int cap, int D, int window,
+                              int sinks, int rolling, float scale, const long long* strides, int layout, int dtype,
+                              void* stream);
+size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, int window, int sinks);
+
 /* Bytes of workspace cattn_attn_bwd needs: 2 * B * H * Sp * sizeof(float),
  * Sp = S rounded up to a multiple of 32 (0 for an empty or invalid shape). */
 size_t cattn_bwd_workspace_bytes(int B, int H, int S, int D);

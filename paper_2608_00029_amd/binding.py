@@ -28,7 +28,10 @@ EXPORTED = ("cattn_attn_fwd", "cattn_attn_bwd", "cattn_attn_fwd_ex", "cattn_attn
             "cattn_attn_bwd_dkdv", "cattn_lmhead_fwd", "cattn_lmhead_workspace_bytes",
             "cattn_bwd_workspace_bytes", "cattn_status_string", "cattn_last_error_string",
             "cattn_layernorm_fwd", "cattn_layernorm_bwd", "cattn_layernorm_bwd_workspace_bytes", "cattn_gelu_fwd",
-            "cattn_gelu_bwd", "cattn_sce_fwd", "cattn_sce_bwd", "cattn_attn_bwd_noalloc")
+            "cattn_gelu_bwd", "cattn_sce_fwd", "cattn_sce_bwd", "cattn_attn_bwd_noalloc",
+            "cattn_rmsnorm_fwd", "cattn_rmsnorm_fwd_q8", "cattn_rmsnorm_bwd", "cattn_rmsnorm_bwd_workspace_bytes",
+            "cattn_rope_frequencies", "cattn_rope", "cattn_rope_append", "cattn_swa_fwd", "cattn_swa_bwd",
+            "cattn_swa_bwd_workspace_bytes", "cattn_swa_decode", "cattn_swa_decode_workspace_bytes")
 
 
 class CattnError(RuntimeError):
@@ -85,6 +88,31 @@ def lib() -> ctypes.CDLL:
         L.cattn_sce_fwd.restype = i
         L.cattn_sce_bwd.argtypes = [vp, vp, vp, f, vp, i, i, vp]
         L.cattn_sce_bwd.restype = i
+        d, lp = ctypes.c_double, ctypes.POINTER(ctypes.c_longlong)
+        L.cattn_rmsnorm_fwd.argtypes = [vp] * 6 + [i, i, f, i, vp]
+        L.cattn_rmsnorm_fwd.restype = i
+        L.cattn_rmsnorm_fwd_q8.argtypes = [vp] * 7 + [i, i, i, f, i, vp]
+        L.cattn_rmsnorm_fwd_q8.restype = i
+        L.cattn_rmsnorm_bwd.argtypes = [vp] * 8 + [i, i, i, vp]
+        L.cattn_rmsnorm_bwd.restype = i
+        L.cattn_rmsnorm_bwd_workspace_bytes.argtypes = [i, i]
+        L.cattn_rmsnorm_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.cattn_rope_frequencies.argtypes = [ctypes.POINTER(d), i, d, i, d, d, d, d]
+        L.cattn_rope_frequencies.restype = i
+        L.cattn_rope.argtypes = [vp] * 6 + [i] * 7 + [lp] + [i] * 3 + [f, i, vp]
+        L.cattn_rope.restype = i
+        L.cattn_rope_append.argtypes = [vp] * 10 + [i] * 10 + [lp, i, i, f, i, vp]
+        L.cattn_rope_append.restype = i
+        L.cattn_swa_fwd.argtypes = [vp] * 6 + [i] * 7 + [f, lp, i, i, vp]
+        L.cattn_swa_fwd.restype = i
+        L.cattn_swa_bwd.argtypes = [vp] * 11 + [i] * 7 + [f, lp, i, i, vp]
+        L.cattn_swa_bwd.restype = i
+        L.cattn_swa_bwd_workspace_bytes.argtypes = [i] * 7
+        L.cattn_swa_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.cattn_swa_decode.argtypes = [vp] * 7 + [i] * 8 + [f, lp, i, i, vp]
+        L.cattn_swa_decode.restype = i
+        L.cattn_swa_decode_workspace_bytes.argtypes = [i] * 7
+        L.cattn_swa_decode_workspace_bytes.restype = ctypes.c_size_t
         L.cattn_status_string.argtypes = [i]
         L.cattn_status_string.restype = ctypes.c_char_p
         L.cattn_last_error_string.argtypes = []

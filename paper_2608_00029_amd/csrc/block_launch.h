@@ -1,0 +1,147 @@
+// Host-side launchers of the decoder-block operators (internal; the public
+// interface is the cattn_rmsnorm_*, cattn_rope* and cattn_swa_* entry points in
+// cattn.h).  Arguments are validated by the caller.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace cattn {
+
+// ---------------------------------------------------------------------------
+// RMSNorm
+// ---------------------------------------------------------------------------
+constexpr int kRmsMaxC = 16384;  // widest row kept in registers (16 waves, 2 x 8 columns a lane)
+
+struct RmsFwd {
+  const void* x;
+  const void* residual;  // or NULL: h is not written
+  const float* gamma;
+  void* y;         // [rows, C] of x's type, or e4m3 codes with `scale`
+  float* scale;    // [rows, groups], 8-bit output only
+  void* h;
+  float* rstd;
+  int rows, C;
+  int group;       // columns of a scale, 8-bit output only
+  float eps;
+  bool bf16;
+};
+struct RmsBwd {
+  const void* h;
+  const float* gamma;
+  const float* rstd;
+  const void* dy;
+  const void* dh;  // or NULL
+  void* dx;
+  float* dgamma;
+  float* part;  // rms_bwd_groups(rows) partial rows of dgamma
+  int rows, C;
+  bool bf16;
+};
+// Work groups of the backward's first kernel; each leaves one partial row of dgamma.
+constexpr int rms_bwd_groups(int rows) { return rows <= 0 ? 0 : (rows + 7) / 8 < 512 ? (rows + 7) / 8 : 512; }
+hipError_t launch_rmsnorm_fwd(const RmsFwd& a, hipStream_t st);
+hipError_t launch_rmsnorm_bwd(const RmsBwd& a, hipStream_t st);
+
+// ---------------------------------------------------------------------------
+// Tensors of heads: the element strides of batch, head and row; a row's columns
+// are consecutive.
+// ---------------------------------------------------------------------------
+struct Strides {
+  int64_t b, h, s;
+};
+
+struct RopeArgs {
+  const void *q, *k, *v;  // v: append only; k may be NULL (Hkv = 0)
+  void *qo, *ko, *kc, *vc;
+  Strides sq, sk, sv, sqo, sko, skc, svc;
+  const int* pos;        // [B, S] (pos_b = S), [S] (pos_b = 0) or NULL: 0 .. S - 1
+  int64_t pos_b;
+  const int* lens;       // append: tokens of each sequence after the call
+  const int* counts;     // append: new tokens of each sequence, or NULL: S
+  const double* freqs;   // [rot / 2] radians per position
+  int B, S, Hq, Hkv, D, rot;
+  float amplitude;
+  bool inverse, interleaved, append, rolling, bf16;
+  bool in_place_q, in_place_k;  // the columns past `rot` are already where they belong
+  int cap, window, sinks;
+};
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------------------
+// Sliding-window attention with sinks
+// ---------------------------------------------------------------------------
+struct SwaArgs {
+  const void *q, *k, *v, *o, *dout;
+  void *out, *dq, *dk, *dv;
+  Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
+  float* lse;       // [B, Hq, S]
+  const int* lens;  // [B] or NULL
+  float* ws;        // [B * Hq][2][ws_rows(S)]: D = rowsum(dO * O) row, then -LSE / scale row
+  float* far;       // partial dK, dV of the sink keys (swa_far_floats)
+  int B, Hq, Hkv, S, D, window, sinks;  // window in [1, S], sinks in [0, S]
+  float scale;
+  bool bf16;
+};
+struct SwaDecodeArgs {
+  const void *q, *k, *v;
+  void* o;
+  Strides sq, sk, sv, so;  // q, o: .s unused
+  float* lse;              // [B, Hq]
+  const int* lens;         // [B]
+  float* ws;               // swa_decode_floats(...)
+  int B, Hq, Hkv, cap, D, window, sinks;
+  float scale;
+  bool rolling, bf16;
+};
+
+constexpr int64_t kSwaCus = 256;  // compute units of the one GPU these kernels are built for
+
+// dK and dV of the sink keys.  Their queries outside the window (`far`: there
+// are some where S > window) reach to the end of the sequence, however long,
+// while every other key has window queries: the far (query head, 32-query tile)
+// pairs of a 32-key tile of sinks are cut into this many parts, so that the
+// parts of all heads give the GPU about two work groups per CU, but a part has
+// at least eight tiles.  Each part leaves float32 partial sums.
+constexpr bool swa_has_far(int S, int window, int sinks) { return sinks > 0 && S > window; }
+constexpr int swa_sink_tiles(int S, int sinks) { return ((sinks < S ? sinks : S) + 31) / 32; }
+constexpr int swa_far_parts(int B, int Hq, int Hkv, int S, int window, int sinks) {
+  if (!swa_has_far(S, window, sinks)) return 0;
+  const int64_t tiles = (int64_t)(Hq / Hkv) * ((S - window + 31) / 32 + 1);
+  const int64_t want = 2 * kSwaCus / ((int64_t)B * Hkv * swa_sink_tiles(S, sinks)), most = (tiles + 7) / 8;
+  const int64_t n = want < most ? want : most;
+  return n < 1 ? 1 : (int)n;
+}
+// Floats of the far area: [B * Hkv][sink tile][1 + parts][dK, dV][32][D]; slot 0
+// is the window's own sum.
+constexpr int64_t swa_far_floats(int B, int Hq, int Hkv, int S, int D, int window, int sinks) {
+  if (!swa_has_far(S, window, sinks)) return 0;
+  return (int64_t)B * Hkv * swa_sink_tiles(S, sinks) * (1 + swa_far_parts(B, Hq, Hkv, S, window, sinks)) * 2 * 32 * D;
+}
+
+// Decoding: parts that the visible slots of one (sequence, key/value head) are
+// cut into.  Each part is a work group of four waves that stream 32-slot tiles;
+// enough of them to give every CU one, but at least four tiles (one per wave)
+// each.
+constexpr int swa_decode_parts(int B, int Hq, int Hkv, int cap, int window, int sinks) {
+  const int64_t row_blocks = (int64_t)B * Hkv * ((Hq / Hkv + 31) / 32);
+  const int64_t seen = (int64_t)window + sinks < cap ? (int64_t)window + sinks : cap;
+  const int64_t most = (seen + 127) / 128, want = (kSwaCus + row_blocks - 1) / row_blocks;
+  const int64_t n = want < most ? want : most;
+  return n < 1 ? 1 : (int)n;
+}
+// Floats of the decode workspace: none for one part, else [part][B * Hq][D + 2].
+constexpr int64_t swa_decode_floats(int B, int Hq, int Hkv, int cap, int D, int window, int sinks) {
+  const int n = swa_decode_parts(B, Hq, Hkv, cap, window, sinks);
+  return n == 1 ? 0 : (int64_t)n * B * Hq * (D + 2);
+}
+
+hipError_t launch_swa_fwd(const SwaArgs& a, hipStream_t st);
+hipError_t launch_swa_bwd(const SwaArgs& a, hipStream_t st);
+hipError_t launch_swa_decode(const SwaDecodeArgs& a, hipStream_t st);
+hipError_t launch_swa_fwd_f32(const SwaArgs& a, hipStream_t st);
+hipError_t launch_swa_bwd_f32(const SwaArgs& a, hipStream_t st);
+// dK, dV of the sink keys from their partial sums (after the kernels that leave them)
+hipError_t launch_swa_far_sum(const SwaArgs& a, hipStream_t st);
+
+}  // namespace cattn

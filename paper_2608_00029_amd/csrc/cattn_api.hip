@@ -10,33 +10,16 @@
 #include <mutex>
 
 #include "../../include/cattn.h"
+#include "api_util.h"
 #include "attn_launch.h"
 #include "lmhead_launch.h"
 #include "memops_launch.h"
 
 extern "C" size_t cattn_bwd_workspace_bytes(int B, int H, int S, int D);
 
+using namespace cattn;
+
 namespace {
-
-thread_local char g_last_error[256] = "";
-
-constexpr float kMinScale = 1e-20f, kMaxScale = 1e6f;
-
-cattn_status fail(cattn_status st, const char* msg) {
-  snprintf(g_last_error, sizeof(g_last_error), "%s", msg);
-  return st;
-}
-
-struct Range {
-  uintptr_t lo, hi;  // [lo, hi)
-};
-
-Range range_of(const void* p, size_t bytes) {
-  const uintptr_t a = (uintptr_t)p;
-  return Range{a, a + bytes};
-}
-
-bool overlap(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; }
 
 // Shape checks shared by both entry points.  Returns CATTN_OK with *empty set
 // when the problem is empty.
@@ -62,25 +45,6 @@ cattn_status check_shape(int B, int H, int S, int D, float scale, int dtype, boo
   if (cattn::fwd_grid_blocks((int)BH, S) >= (int64_t(1) << 31) || cattn::bwd_grid_blocks((int)BH, S) >= (int64_t(1) << 31))
     return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
   return CATTN_OK;
-}
-
-cattn_status hip_status(hipError_t e) {
-  if (e == hipSuccess) return CATTN_OK;
-  snprintf(g_last_error, sizeof(g_last_error), "HIP error %d: %s", (int)e, hipGetErrorString(e));
-  return CATTN_ERR_HIP;
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-// Every output range against every input range and against the other outputs.
-bool any_overlap(const Range* ins, int ni, const Range* outs, int no) {
-  for (int i = 0; i < no; ++i) {
-    for (int j = 0; j < ni; ++j)
-      if (overlap(outs[i], ins[j])) return true;
-    for (int j = i + 1; j < no; ++j)
-      if (overlap(outs[i], outs[j])) return true;
-  }
-  return false;
 }
 
 }  // namespace

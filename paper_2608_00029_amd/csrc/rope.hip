@@ -1,0 +1,243 @@
+// Rotary positions of queries and keys, and the append of rotated keys and of
+// values to a cache, for gfx950.
+//
+// Pair i of a head at position p turns by the angle p f_i:
+//     (a, b) -> amplitude (a cos - b sin, b cos + a sin)
+// (the backward turns by -p f_i).  Bound by memory: q and k are read and
+// written once.  A work group takes a few tokens: it first forms their sines
+// and cosines, one per token and pair, in LDS, and all heads then share them.
+//
+// Angles: p f / 2 pi is formed in 64 bits and its whole turns are dropped there,
+// so that far positions keep their angle (a 32-bit product is off by 0.06
+// radians at position 10^6); the rest, at most half a turn, goes to 32 bits.
+#include "attn_device.h"
+#include "attn_launch.h"
+#include "block_launch.h"
+
+namespace cattn {
+
+namespace {
+
+constexpr int kMaxTokens = 8;     // tokens of a work group
+constexpr int kRopeTable = 256;   // (token, pair) entries of its table
+
+// V consecutive elements; V = 16 bytes' worth is one access.
+template <typename T, int V> __device__ __forceinline__ void load_v(const T* p, float (&f)[V]) {
+  if constexpr (sizeof(T) == 2 && V == 8) {
+    const bf16x8 v = *(const bf16x8*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
+  } else if constexpr (sizeof(T) == 4 && V == 4) {
+    const f32x4 v = *(const f32x4*)p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = v[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = (float)p[e];
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void store_v(T* p, const float (&f)[V]) {
+  if constexpr (sizeof(T) == 2 && V == 8) {
+    bf16x8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (__bf16)f[e];
+    *(bf16x8*)p = v;
+  } else if constexpr (sizeof(T) == 4 && V == 4) {
+    *(f32x4*)p = f32x4{f[0], f[1], f[2], f[3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) p[e] = (T)f[e];
+  }
+}
+
+struct Token {
+  int b, s;
+  int slot;    // append: where the cache takes it, or -1
+  int active;  // append: it has a position
+};
+
+// Slot of position p in the cache of a sequence of `len` tokens, or -1 where it
+// is not kept: a rolling cache keeps the sinks and the last `window` positions.
+__device__ __forceinline__ int cache_slot(int p, int len, const RopeArgs& a) {
+  if (!a.rolling) return p < a.cap ? p : -1;
+  if (p < a.sinks) return p;
+  return p >= len - a.window ? a.sinks + (p - a.sinks) % a.window : -1;
+}
+
+// Items of a head's row: the rotated part in steps of V pairs (half layout) or
+// V / 2 pairs (interleaved), then the rest in steps of V columns.
+template <typename T, int V, bool INTER, bool APPEND>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int tpg, int items, int rot_items) {
+  __shared__ float cs[kRopeTable], sn[kRopeTable];
+  __shared__ Token tok[kMaxTokens];
+  const int tid = threadIdx.x, half = a.rot >> 1;
+  const int64_t total = (int64_t)a.B * a.S, first = (int64_t)blockIdx.x * tpg;
+  const int n_tok = (int)(total - first < tpg ? total - first : tpg);
+
+  auto place = [&](int t, Token& k) {  // token t of this work group; returns its position
+    const int64_t at = first + t;
+    k.b = (int)(at / a.S);
+    k.s = (int)(at - (int64_t)k.b * a.S);
+    k.slot = -1;
+    k.active = 1;
+    if constexpr (APPEND) {
+      const int len = max(a.lens[k.b], 0);
+      const int n = a.counts ? min(max(a.counts[k.b], 0), a.S) : a.S;
+      const int p = len - n + k.s;
+      k.active = k.s < n && p >= 0;
+      if (k.active) k.slot = cache_slot(p, len, a);
+      return k.active ? p : 0;
+    } else {
+      return a.pos ? a.pos[k.b * a.pos_b + k.s] : k.s;
+    }
+  };
+  constexpr double kPerTurn = 0.15915494309189533577;  // 1 / (2 pi)
+  for (int i = tid; i < n_tok * half; i += 256) {
+    const int t = i / half;
+    Token k;
+    const double turns = (double)place(t, k) * (a.freqs[i - t * half] * kPerTurn);
+    float s, c;
+    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+    cs[i] = c * a.amplitude;
+    sn[i] = (a.inverse ? -s : s) * a.amplitude;
+  }
+  if (tid < n_tok) {
+    Token k;
+    place(tid, k);
+    tok[tid] = k;
+  }
+  __syncthreads();
+
+  // `wide` threads a row; a row is one head of one token
+  const int wide = min(items, 256), rows_at_once = 256 / wide;
+  const int c0 = tid % wide, r0 = tid / wide;
+  if (r0 >= rows_at_once) return;
+  const int heads = a.Hq + a.Hkv;
+  int t = r0 / heads, head = r0 - t * heads;
+  const int dt = rows_at_once / heads, dh = rows_at_once - dt * heads;
+  for (; t < n_tok;) {
+    const Token k = tok[t];
+    const bool is_q = head < a.Hq;
+    const int hh = is_q ? head : head - a.Hq;
+    const Strides si = is_q ? a.sq : a.sk, so = is_q ? a.sqo : a.sko;
+    const T* src = (const T*)(is_q ? a.q : a.k) + k.b * si.b + hh * si.h + k.s * si.s;
+    T* dst = (T*)(is_q ? a.qo : a.ko) + k.b * so.b + hh * so.h + k.s * so.s;
+    T* cache = nullptr;
+    if (APPEND && !is_q && k.slot >= 0) cache = (T*)a.kc + k.b * a.skc.b + hh * a.skc.h + k.slot * a.skc.s;
+    const bool keep_rest = is_q ? a.in_place_q : a.in_place_k;
+    for (int c = c0; c < items; c += wide) {
+      if (c >= rot_items) {  // columns past the rotated part
+        const int col = a.rot + (c - rot_items) * V;
+        if (keep_rest && !cache && k.active) continue;
+        float x[V];
+        load_v<T, V>(src + col, x);
+        if (APPEND && !k.active) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) x[e] = 0.f;
+        }
+        if (!keep_rest || !k.active) store_v<T, V>(dst + col, x);
+        if (cache) store_v<T, V>(cache + col, x);
+      } else if constexpr (INTER) {
+        const int col = c * V, f = t * half + c * (V / 2);
+        float x[V], y[V];
+        load_v<T, V>(src + col, x);
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const float co = cs[f + e / 2], s = sn[f + e / 2];
+          y[e] = x[e] * co - x[e + 1] * s;
+          y[e + 1] = x[e + 1] * co + x[e] * s;
+        }
+        if (APPEND && !k.active) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) y[e] = 0.f;
+        }
+        store_v<T, V>(dst + col, y);
+        if (cache) store_v<T, V>(cache + col, y);
+      } else {
+        const int col = c * V, f = t * half + col;
+        float x[V], u[V], y[V], z[V];
+        load_v<T, V>(src + col, x);
+        load_v<T, V>(src + col + half, u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float co = cs[f + e], s = sn[f + e];
+          y[e] = x[e] * co - u[e] * s;
+          z[e] = u[e] * co + x[e] * s;
+        }
+        if (APPEND && !k.active) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) y[e] = z[e] = 0.f;
+        }
+        store_v<T, V>(dst + col, y);
+        store_v<T, V>(dst + col + half, z);
+        if (cache) {
+          store_v<T, V>(cache + col, y);
+          store_v<T, V>(cache + col + half, z);
+        }
+      }
+    }
+    t += dt;
+    head += dh;
+    if (head >= heads) {
+      head -= heads;
+      ++t;
+    }
+  }
+  if constexpr (APPEND) {  // values
+    const int n = a.D / V;
+    for (int i = tid; i < n_tok * a.Hkv * n; i += rows_at_once * wide) {
+      const int row = i / n, col = (i - row * n) * V, tt = row / a.Hkv, hh = row - tt * a.Hkv;
+      const Token k = tok[tt];
+      if (k.slot < 0) continue;
+      float x[V];
+      load_v<T, V>((const T*)a.v + k.b * a.sv.b + hh * a.sv.h + k.s * a.sv.s + col, x);
+      store_v<T, V>((T*)a.vc + k.b * a.svc.b + hh * a.svc.h + k.slot * a.svc.s + col, x);
+    }
+  }
+}
+
+template <typename T, int V, bool INTER> hipError_t rope_v(const RopeArgs& a, hipStream_t st) {
+  const int half = a.rot / 2;
+  const int rot_items = INTER ? a.rot / V : half / V, items = rot_items + (a.D - a.rot) / V;
+  // As many tokens a work group as fill its threads once with sines, where
+  // there are enough for the GPU's work groups all the same.
+  const int64_t total = (int64_t)a.B * a.S;
+  int tpg = 256 / half;
+  tpg = tpg < 1 ? 1 : tpg > kMaxTokens ? kMaxTokens : tpg;
+  while (tpg > 1 && total < (int64_t)tpg * 8 * cu_count()) tpg /= 2;
+  const dim3 grid((unsigned)((total + tpg - 1) / tpg));
+  if (a.append) hipLaunchKernelGGL((rope_kernel<T, V, INTER, true>), grid, dim3(256), 0, st, a, tpg, items, rot_items);
+  else hipLaunchKernelGGL((rope_kernel<T, V, INTER, false>), grid, dim3(256), 0, st, a, tpg, items, rot_items);
+  return hipGetLastError();
+}
+
+bool wide_strides(const Strides& s, int v) { return s.b % v == 0 && s.h % v == 0 && s.s % v == 0; }
+bool wide_pointer(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Whether every access can be 16 bytes: the columns of each item, the strides
+// and the addresses; else element by element.
+template <typename T> bool rope_wide(const RopeArgs& a) {
+  constexpr int V = 16 / sizeof(T);
+  if ((a.interleaved ? a.rot : a.rot / 2) % V || (a.D - a.rot) % V) return false;
+  bool ok = wide_strides(a.sq, V) && wide_strides(a.sqo, V) && wide_pointer(a.q) && wide_pointer(a.qo);
+  if (a.Hkv)
+    ok = ok && wide_strides(a.sk, V) && wide_strides(a.sko, V) && wide_pointer(a.k) && wide_pointer(a.ko);
+  if (a.append)
+    ok = ok && wide_strides(a.sv, V) && wide_strides(a.skc, V) && wide_strides(a.svc, V) && wide_pointer(a.v) &&
+         wide_pointer(a.kc) && wide_pointer(a.vc);
+  return ok;
+}
+
+template <typename T> hipError_t rope_t(const RopeArgs& a, hipStream_t st) {
+  constexpr int V = 16 / sizeof(T);
+  if (rope_wide<T>(a)) return a.interleaved ? rope_v<T, V, true>(a, st) : rope_v<T, V, false>(a, st);
+  return a.interleaved ? rope_v<T, 2, true>(a, st) : rope_v<T, 1, false>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st) {
+  return a.bf16 ? rope_t<__bf16>(a, st) : rope_t<float>(a, st);
+}
+
+}  // namespace cattn
