@@ -26,13 +26,14 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <typename T> struct Io;
 template <> struct Io<__bf16> {
   typedef bf16x8 vec;
-  static __device__ __forceinline__ f32x8 load(const void* p, int64_t i) {
-    const vec v = *((const vec*)p + i);
+  static __device__ __forceinline__ vec raw(const void* p, int64_t i) { return *((const vec*)p + i); }
+  static __device__ __forceinline__ f32x8 wide(const vec& v) {
     f32x8 f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
     return f;
   }
+  static __device__ __forceinline__ f32x8 load(const void* p, int64_t i) { return wide(raw(p, i)); }
   static __device__ __forceinline__ void store(void* p, int64_t i, const f32x8& f) {
     vec v;
 #pragma unroll
@@ -41,10 +42,13 @@ template <> struct Io<__bf16> {
   }
 };
 template <> struct Io<float> {
-  static __device__ __forceinline__ f32x8 load(const void* p, int64_t i) {
+  typedef f32x8 vec;
+  static __device__ __forceinline__ vec raw(const void* p, int64_t i) {
     const f32x4 a = ((const f32x4*)p)[2 * i], b = ((const f32x4*)p)[2 * i + 1];
     return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   }
+  static __device__ __forceinline__ f32x8 wide(const vec& v) { return v; }
+  static __device__ __forceinline__ f32x8 load(const void* p, int64_t i) { return raw(p, i); }
   static __device__ __forceinline__ void store(void* p, int64_t i, const f32x8& f) {
     __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, (f32x4*)p + 2 * i);
     __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, (f32x4*)p + 2 * i + 1);
@@ -209,33 +213,54 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void rmsnorm_bwd_kernel(RmsBw
     g[k] = c < C8 ? Io<float>::load(a.gamma, c) : f32x8{};
     dg[k] = f32x8{};
   }
-  int par = 0;
-  for (int64_t row = r0 + w / W; row < r1; row += RPG, par ^= 1) {
-    const int64_t base = row * C8;
-    f32x8 v[N], d[N];
+  // One row ahead: a row's loads are in flight while the one before it is
+  // reduced and stored.  (Not at two steps of 16 waves, whose 128 registers a
+  // lane have no room for a second row.)
+  constexpr bool AHEAD = !(W == 16 && N == 2);
+  typedef typename Io<T>::vec Raw;
+  Raw hn[N], dn[N], un[N];
+  float rn = 0.f;
+  auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const int c = lane + 64 * (wr + W * k);
-      v[k] = c < C8 ? Io<T>::load(a.h, base + c) : f32x8{};
-      d[k] = c < C8 ? Io<T>::load(a.dy, base + c) : f32x8{};
+      if (c < C8) {
+        hn[k] = Io<T>::raw(a.h, row * C8 + c);
+        dn[k] = Io<T>::raw(a.dy, row * C8 + c);
+        if constexpr (DH) un[k] = Io<T>::raw(a.dh, row * C8 + c);
+      }
     }
-    const float rs = a.rstd[row];
+    rn = a.rstd[row];
+  };
+#pragma unroll
+  for (int k = 0; k < N; ++k) hn[k] = dn[k] = un[k] = Raw{};
+  int par = 0;
+  int64_t row = r0 + w / W;
+  if (AHEAD && row < r1) fetch(row);
+  for (; row < r1; row += RPG, par ^= 1) {
+    if (!AHEAD) fetch(row);
+    f32x8 v[N], d[N];
+    Raw u[N];
+    const float rs = rn;
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      v[k] *= rs;
+      v[k] = Io<T>::wide(hn[k]) * rs;
+      d[k] = Io<T>::wide(dn[k]);
+      u[k] = un[k];
       dg[k] += d[k] * v[k];
       d[k] *= g[k];
       s += sum8(d[k] * v[k]);
     }
+    if (AHEAD && row + RPG < r1) fetch(row + RPG);
     const float mean = row_sum<W>(s, red[par], wr) / fc;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const int c = lane + 64 * (wr + W * k);
       if (c < C8) {
         f32x8 o = (d[k] - v[k] * mean) * rs;
-        if constexpr (DH) o += Io<T>::load(a.dh, base + c);
-        Io<T>::store(a.dx, base + c, o);
+        if constexpr (DH) o += Io<T>::wide(u[k]);
+        Io<T>::store(a.dx, row * C8 + c, o);
       }
     }
   }
@@ -343,7 +368,7 @@ template <typename T> hipError_t fwd_t(const RmsFwd& a, hipStream_t st) {
 template <typename T, int W> hipError_t bwd_w(const RmsBwd& a, hipStream_t st) {
   constexpr int WG = W == 16 ? 16 : 4;
   const dim3 grid((unsigned)rms_bwd_groups(a.rows)), block(WG * 64);
-  return by_steps<W, W == 1 ? 1 : 2, most_steps(W)>(a.C, [&](auto n) {
+  return by_steps<W, 1, 2>(a.C, [&](auto n) {
     constexpr int N = decltype(n)::value;
     if (a.dh) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, W, N, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, W, N, false>), grid, block, 0, st, a);
@@ -353,7 +378,7 @@ template <typename T, int W> hipError_t bwd_w(const RmsBwd& a, hipStream_t st) {
 
 template <typename T> hipError_t bwd_t(const RmsBwd& a, hipStream_t st) {
   const int oct = a.C / 8;
-  hipError_t e = oct <= 4 * 64 ? bwd_w<T, 1>(a, st) : oct <= 16 * 64 ? bwd_w<T, 4>(a, st) : bwd_w<T, 16>(a, st);
+  hipError_t e = oct <= 2 * 64 ? bwd_w<T, 1>(a, st) : oct <= 8 * 64 ? bwd_w<T, 4>(a, st) : bwd_w<T, 16>(a, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(rmsnorm_bwd_sum_kernel, dim3((unsigned)((a.C / 4 + 7) / 8)), dim3(1024), 0, st,
                      (const float*)a.part, a.dgamma, rms_bwd_groups(a.rows), a.C);
