@@ -22,32 +22,38 @@ constexpr int kMaxTokens = 8;     // tokens of a work group
 constexpr int kRopeTable = 256;   // (token, pair) entries of its table
 
 // V consecutive elements; V = 16 bytes' worth is one access.
-template <typename T, int V> __device__ __forceinline__ void load_v(const T* p, float (&f)[V]) {
+template <int V> struct Floats { typedef float type __attribute__((ext_vector_type(V))); };
+template <typename T, int V> __device__ __forceinline__ typename Floats<V>::type load_v(const T* p) {
+  typename Floats<V>::type f;
   if constexpr (sizeof(T) == 2 && V == 8) {
     const bf16x8 v = *(const bf16x8*)p;
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
   } else if constexpr (sizeof(T) == 4 && V == 4) {
-    const f32x4 v = *(const f32x4*)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = v[e];
+    f = *(const f32x4*)p;
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) f[e] = (float)p[e];
   }
+  return f;
 }
-template <typename T, int V> __device__ __forceinline__ void store_v(T* p, const float (&f)[V]) {
+template <typename T, int V> __device__ __forceinline__ void store_v(T* p, typename Floats<V>::type f) {
   if constexpr (sizeof(T) == 2 && V == 8) {
     bf16x8 v;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (__bf16)f[e];
     *(bf16x8*)p = v;
   } else if constexpr (sizeof(T) == 4 && V == 4) {
-    *(f32x4*)p = f32x4{f[0], f[1], f[2], f[3]};
+    *(f32x4*)p = f;
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) p[e] = (T)f[e];
   }
+}
+
+// (field by field: a choice between two structs would go through memory)
+__device__ __forceinline__ Strides choose(bool first, const Strides& x, const Strides& y) {
+  return Strides{first ? x.b : y.b, first ? x.h : y.h, first ? x.s : y.s};
 }
 
 struct Token {
@@ -65,7 +71,9 @@ __device__ __forceinline__ int cache_slot(int p, int len, const RopeArgs& a) {
 }
 
 // Items of a head's row: the rotated part in steps of V pairs (half layout) or
-// V / 2 pairs (interleaved), then the rest in steps of V columns.
+// V / 2 pairs (interleaved), then the rest in steps of V columns.  A row is one
+// head of one token; the work groups (x, y), y = 0 .. gridDim.y - 1, share the
+// rows of their tokens.
 template <typename T, int V, bool INTER, bool APPEND>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int tpg, int items, int rot_items) {
   __shared__ float cs[kRopeTable], sn[kRopeTable];
@@ -91,14 +99,55 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int tpg, int item
       return a.pos ? a.pos[k.b * a.pos_b + k.s] : k.s;
     }
   };
+
+  // `wide` threads a row, as many rows at once as 256 threads give
+  const int wide = min(items, 256), rows_at_once = 256 / wide;
+  const int c0 = tid % wide, r0 = tid / wide;
+  const int heads = a.Hq + a.Hkv, step = rows_at_once * gridDim.y;
+  const int dt = step / heads, dh = step - dt * heads;
+  int c = c0, t = (r0 + rows_at_once * blockIdx.y) / heads, head = r0 + rows_at_once * blockIdx.y - t * heads;
+  bool live = r0 < rows_at_once && t < n_tok;
+
+  // The columns of the present item, x, and in the half layout u, the other half
+  // of its pairs.
+  typedef typename Floats<V>::type Vec;
+  Vec x{}, u{};
+  auto source = [&](int b, int s) {
+    const bool is_q = head < a.Hq;
+    const Strides si = choose(is_q, a.sq, a.sk);
+    return (const T*)(is_q ? a.q : a.k) + b * si.b + (is_q ? head : head - a.Hq) * si.h + s * si.s;
+  };
+  // (columns past the rotated part have no other half: u is then the item again)
+  auto column = [&] { return c < rot_items ? c * V : a.rot + (c - rot_items) * V; };
+  auto other = [&] { return c < rot_items ? c * V + half : a.rot + (c - rot_items) * V; };
+  // The first item is on its way while the sines are formed: a call of few
+  // tokens is a chain of latencies.
+  if (live) {
+    const int64_t at = first + t;
+    const int b = (int)(at / a.S);
+    const T* src = source(b, (int)(at - (int64_t)b * a.S));
+    x = load_v<T, V>(src + column());
+    if constexpr (!INTER) u = load_v<T, V>(src + other());
+  }
+  if constexpr (APPEND) {  // values
+    const int n = a.D / V;
+    for (int i = tid + 256 * blockIdx.y; i < n_tok * a.Hkv * n; i += 256 * gridDim.y) {
+      const int row = i / n, col = (i - row * n) * V, tt = row / a.Hkv, hh = row - tt * a.Hkv;
+      Token k;
+      place(tt, k);
+      if (k.slot < 0) continue;
+      const auto w = load_v<T, V>((const T*)a.v + k.b * a.sv.b + hh * a.sv.h + k.s * a.sv.s + col);
+      store_v<T, V>((T*)a.vc + k.b * a.svc.b + hh * a.svc.h + k.slot * a.svc.s + col, w);
+    }
+  }
   constexpr double kPerTurn = 0.15915494309189533577;  // 1 / (2 pi)
   for (int i = tid; i < n_tok * half; i += 256) {
-    const int t = i / half;
+    const int tt = i / half;
     Token k;
-    const double turns = (double)place(t, k) * (a.freqs[i - t * half] * kPerTurn);
-    float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-    cs[i] = c * a.amplitude;
+    const double turns = (double)place(tt, k) * (a.freqs[i - tt * half] * kPerTurn);
+    float s, co;
+    sincospif((float)(2.0 * (turns - rint(turns))), &s, &co);
+    cs[i] = co * a.amplitude;
     sn[i] = (a.inverse ? -s : s) * a.amplitude;
   }
   if (tid < n_tok) {
@@ -108,90 +157,60 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int tpg, int item
   }
   __syncthreads();
 
-  // `wide` threads a row; a row is one head of one token
-  const int wide = min(items, 256), rows_at_once = 256 / wide;
-  const int c0 = tid % wide, r0 = tid / wide;
-  if (r0 >= rows_at_once) return;
-  const int heads = a.Hq + a.Hkv;
-  int t = r0 / heads, head = r0 - t * heads;
-  const int dt = rows_at_once / heads, dh = rows_at_once - dt * heads;
-  for (; t < n_tok;) {
+  while (live) {
     const Token k = tok[t];
     const bool is_q = head < a.Hq;
     const int hh = is_q ? head : head - a.Hq;
-    const Strides si = is_q ? a.sq : a.sk, so = is_q ? a.sqo : a.sko;
-    const T* src = (const T*)(is_q ? a.q : a.k) + k.b * si.b + hh * si.h + k.s * si.s;
+    const Strides so = choose(is_q, a.sqo, a.sko);
     T* dst = (T*)(is_q ? a.qo : a.ko) + k.b * so.b + hh * so.h + k.s * so.s;
     T* cache = nullptr;
     if (APPEND && !is_q && k.slot >= 0) cache = (T*)a.kc + k.b * a.skc.b + hh * a.skc.h + k.slot * a.skc.s;
-    const bool keep_rest = is_q ? a.in_place_q : a.in_place_k;
-    for (int c = c0; c < items; c += wide) {
-      if (c >= rot_items) {  // columns past the rotated part
-        const int col = a.rot + (c - rot_items) * V;
-        if (keep_rest && !cache && k.active) continue;
-        float x[V];
-        load_v<T, V>(src + col, x);
-        if (APPEND && !k.active) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) x[e] = 0.f;
-        }
-        if (!keep_rest || !k.active) store_v<T, V>(dst + col, x);
-        if (cache) store_v<T, V>(cache + col, x);
-      } else if constexpr (INTER) {
-        const int col = c * V, f = t * half + c * (V / 2);
-        float x[V], y[V];
-        load_v<T, V>(src + col, x);
+    const bool turned = c < rot_items;
+    const int col = column();
+    Vec y = x, z = u;
+    if (turned) {
+      const int f = t * half + (INTER ? c * (V / 2) : c * V);
+      if constexpr (INTER) {
 #pragma unroll
         for (int e = 0; e < V; e += 2) {
           const float co = cs[f + e / 2], s = sn[f + e / 2];
           y[e] = x[e] * co - x[e + 1] * s;
           y[e + 1] = x[e + 1] * co + x[e] * s;
         }
-        if (APPEND && !k.active) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) y[e] = 0.f;
-        }
-        store_v<T, V>(dst + col, y);
-        if (cache) store_v<T, V>(cache + col, y);
       } else {
-        const int col = c * V, f = t * half + col;
-        float x[V], u[V], y[V], z[V];
-        load_v<T, V>(src + col, x);
-        load_v<T, V>(src + col + half, u);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float co = cs[f + e], s = sn[f + e];
           y[e] = x[e] * co - u[e] * s;
           z[e] = u[e] * co + x[e] * s;
         }
-        if (APPEND && !k.active) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) y[e] = z[e] = 0.f;
-        }
-        store_v<T, V>(dst + col, y);
-        store_v<T, V>(dst + col + half, z);
-        if (cache) {
-          store_v<T, V>(cache + col, y);
-          store_v<T, V>(cache + col + half, z);
-        }
       }
     }
-    t += dt;
-    head += dh;
-    if (head >= heads) {
-      head -= heads;
-      ++t;
+    if (APPEND && !k.active) y = z = Vec{};
+    const bool two = !INTER && turned;
+    if (turned || !(is_q ? a.in_place_q : a.in_place_k) || !k.active) {  // (else it is where it belongs)
+      store_v<T, V>(dst + col, y);
+      if (two) store_v<T, V>(dst + col + half, z);
     }
-  }
-  if constexpr (APPEND) {  // values
-    const int n = a.D / V;
-    for (int i = tid; i < n_tok * a.Hkv * n; i += rows_at_once * wide) {
-      const int row = i / n, col = (i - row * n) * V, tt = row / a.Hkv, hh = row - tt * a.Hkv;
-      const Token k = tok[tt];
-      if (k.slot < 0) continue;
-      float x[V];
-      load_v<T, V>((const T*)a.v + k.b * a.sv.b + hh * a.sv.h + k.s * a.sv.s + col, x);
-      store_v<T, V>((T*)a.vc + k.b * a.svc.b + hh * a.svc.h + k.slot * a.svc.s + col, x);
+    if (APPEND && cache) {
+      store_v<T, V>(cache + col, y);
+      if (two) store_v<T, V>(cache + col + half, z);
+    }
+    c += wide;
+    if (c >= items) {
+      c = c0;
+      t += dt;
+      head += dh;
+      if (head >= heads) {
+        head -= heads;
+        ++t;
+      }
+      live = t < n_tok;
+    }
+    if (live) {
+      const T* src = source(tok[t].b, tok[t].s);
+      x = load_v<T, V>(src + column());
+      if constexpr (!INTER) u = load_v<T, V>(src + other());
     }
   }
 }
@@ -205,7 +224,13 @@ template <typename T, int V, bool INTER> hipError_t rope_v(const RopeArgs& a, hi
   int tpg = 256 / half;
   tpg = tpg < 1 ? 1 : tpg > kMaxTokens ? kMaxTokens : tpg;
   while (tpg > 1 && total < (int64_t)tpg * 8 * cu_count()) tpg /= 2;
-  const dim3 grid((unsigned)((total + tpg - 1) / tpg));
+  // Few tokens: their heads over more work groups, until a thread has one item
+  // or the GPU its work groups.
+  const int64_t groups = (total + tpg - 1) / tpg;
+  const int64_t passes = ((int64_t)tpg * (a.Hq + a.Hkv) * items + 255) / 256;
+  int64_t shares = 2 * cu_count() / groups;
+  shares = shares < 1 ? 1 : shares < passes ? shares : passes;
+  const dim3 grid((unsigned)groups, (unsigned)shares);
   if (a.append) hipLaunchKernelGGL((rope_kernel<T, V, INTER, true>), grid, dim3(256), 0, st, a, tpg, items, rot_items);
   else hipLaunchKernelGGL((rope_kernel<T, V, INTER, false>), grid, dim3(256), 0, st, a, tpg, items, rot_items);
   return hipGetLastError();
