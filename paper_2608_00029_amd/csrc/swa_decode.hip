@@ -100,8 +100,8 @@ __device__ __forceinline__ Place place_of(const SwaDecodeArgs& a) {
 
 // The four waves' (O, offset, sum) meet in `area`; each wave finishes a quarter
 // of the columns: column index groups g = w of every column block.  With one
-// part that is O and LSE, else the part's row of the workspace
-// ([part][B * Hq][D + 2]: O at the offset, then offset times c and sum).
+// part that is O and LSE, else the part's rows of the workspace: O at the
+// offset [part][B * Hq][D], then offset times c, and sum [part][B * Hq][2].
 template <int D, typename T, typename Store>
 __device__ __forceinline__ void finish(const SwaDecodeArgs& a, const Place& pl, f32x4* area, float (*stats)[4][64],
                                        int w, int lane, const f32x16 (&acc)[D / 32], const Running& run, float c,
@@ -134,12 +134,9 @@ __device__ __forceinline__ void finish(const SwaDecodeArgs& a, const Place& pl, 
   }
   const int bh = pl.bh0 + r;
   if (parts > 1) {
-    float* o = a.ws + ((int64_t)pl.part * a.B * a.Hq + bh) * (D + 2);
-    store((T*)nullptr, o, v, 1.f);
-    if (w == 0 && h == 0) {
-      o[D] = mn * c;
-      o[D + 1] = l;
-    }
+    const int64_t heads = (int64_t)a.B * a.Hq, at = pl.part * heads + bh;
+    store((T*)nullptr, a.ws + at * D, v, 1.f);
+    if (w == 0 && h == 0) *(f32x2*)(a.ws + parts * heads * D + 2 * at) = f32x2{mn * c, l};
   } else {
     store((T*)a.o + pl.b * a.so.b + (pl.row0 + r) * a.so.h, (float*)nullptr, v, l > 0.f ? 1.f / l : 0.f);
     if (w == 0 && h == 0) a.lse[bh] = l > 0.f ? (mn * c + log2f(l)) * kLn2 : l == 0.f ? -INFINITY : l;
@@ -238,12 +235,8 @@ __global__ __launch_bounds__(256) void swa_decode_bf16_kernel(SwaDecodeArgs a, f
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
                       const int col = dt * 32 + 8 * w + 4 * h;
-                      if (part) {  // rows of D + 2 floats: 8-byte aligned
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) part[col + e] = v[dt][e];
-                      } else {
-                        store4<bf16>(o + col, v[dt][0] * f, v[dt][1] * f, v[dt][2] * f, v[dt][3] * f);
-                      }
+                      if (part) *(f32x4*)(part + col) = v[dt];
+                      else store4<bf16>(o + col, v[dt][0] * f, v[dt][1] * f, v[dt][2] * f, v[dt][3] * f);
                     }
                   });
 }
@@ -308,25 +301,45 @@ __global__ __launch_bounds__(256) void swa_decode_f32_kernel(SwaDecodeArgs a, fl
                    });
 }
 
-// The parts of one query head, joined in order by D threads.
+// The parts of one query head.  Thread t weighs part t (parts <= 256); then a
+// thread takes four columns of every n-th part, n = 256 / (D / 4), and the n sums
+// are added in order.
 template <typename T>
-__global__ __launch_bounds__(128) void swa_decode_join_kernel(SwaDecodeArgs a, int parts) {
-  const int bh = blockIdx.x, b = bh / a.Hq, hq = bh - b * a.Hq, d = threadIdx.x;
-  const int64_t step = (int64_t)a.B * a.Hq * (a.D + 2);
-  const float* p = a.ws + (int64_t)bh * (a.D + 2);
-  float m = -INFINITY;
-  for (int i = 0; i < parts; ++i)
-    if (p[i * step + a.D + 1] > 0.f) m = fmaxf(m, p[i * step + a.D]);
-  float l = 0.f, o = 0.f;
-  for (int i = 0; i < parts; ++i) {
-    const float li = p[i * step + a.D + 1];
-    if (li == 0.f) continue;  // saw no slot
-    const float f = exp2_hw(p[i * step + a.D] - m);
-    l += li * f;
-    o += p[i * step + d] * f;
+__global__ __launch_bounds__(256) void swa_decode_join_kernel(SwaDecodeArgs a, int parts) {
+  __shared__ float weight[256], red[2][4];
+  __shared__ f32x4 sums[256];
+  const int tid = threadIdx.x, w = tid >> 6;
+  const int bh = blockIdx.x, b = bh / a.Hq, hq = bh - b * a.Hq;
+  const int64_t heads = (int64_t)a.B * a.Hq;
+  const int quads = a.D / 4, n = 256 / quads, q = tid % quads, s0 = tid / quads;
+  const f32x4* p = (const f32x4*)a.ws + (int64_t)bh * quads + q;
+  f32x2 st{0.f, 0.f};
+  if (tid < parts) st = *(const f32x2*)(a.ws + parts * heads * a.D + 2 * (tid * heads + bh));
+  const float m = wave_max(st[1] == 0.f ? -INFINITY : st[0]);  // (sum 0: the part saw no slot)
+  if ((tid & 63) == 0) red[0][w] = m;
+  __syncthreads();
+  const float mm = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  const float f = st[1] == 0.f ? 0.f : exp2_hw(st[0] - mm);
+  weight[tid] = f;
+  const float sum = wave_sum(st[1] * f);
+  if ((tid & 63) == 0) red[1][w] = sum;
+  __syncthreads();
+  const float l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  f32x4 v{};
+#pragma unroll 4
+  for (int s = s0; s < parts; s += n) {
+    const float g = weight[s];
+    if (g != 0.f) v += p[(int64_t)s * heads * quads] * g;  // (a part without slots holds 0 at weight 0: not read)
   }
-  ((T*)a.o)[b * a.so.b + hq * a.so.h + d] = (T)(l == 0.f ? 0.f : o / l);
-  if (d == 0) a.lse[bh] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  sums[tid] = v;
+  __syncthreads();
+  if (s0) return;
+  for (int i = 1; i < n; ++i) v += sums[i * quads + q];
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* o = (T*)a.o + b * a.so.b + hq * a.so.h + 4 * q;
+  if constexpr (sizeof(T) == 2) store4<bf16>(o, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  else *(f32x4*)o = v * inv;
+  if (tid == 0) a.lse[bh] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
 }
 
 }  // namespace
@@ -346,8 +359,8 @@ hipError_t launch_swa_decode(const SwaDecodeArgs& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   const dim3 heads((unsigned)(a.B * a.Hq));
-  if (a.bf16) hipLaunchKernelGGL((swa_decode_join_kernel<bf16>), heads, dim3(a.D), 0, st, a, parts);
-  else hipLaunchKernelGGL((swa_decode_join_kernel<float>), heads, dim3(a.D), 0, st, a, parts);
+  if (a.bf16) hipLaunchKernelGGL((swa_decode_join_kernel<bf16>), heads, dim3(256), 0, st, a, parts);
+  else hipLaunchKernelGGL((swa_decode_join_kernel<float>), heads, dim3(256), 0, st, a, parts);
   return hipGetLastError();
 }
 
