@@ -101,14 +101,15 @@ constexpr int64_t kSwaCus = 256;  // compute units of the one GPU these kernels 
 // are some where S > window) reach to the end of the sequence, however long,
 // while every other key has window queries: the far (query head, 32-query tile)
 // pairs of a 32-key tile of sinks are cut into this many parts, so that the
-// parts of all heads give the GPU about two work groups per CU, but a part has
-// at least eight tiles.  Each part leaves float32 partial sums.
+// parts of all heads give the GPU one work group per CU (what its LDS holds at D
+// = 128), but a part has at least eight tiles.  Each part leaves float32 partial
+// sums.
 constexpr bool swa_has_far(int S, int window, int sinks) { return sinks > 0 && S > window; }
 constexpr int swa_sink_tiles(int S, int sinks) { return ((sinks < S ? sinks : S) + 31) / 32; }
 constexpr int swa_far_parts(int B, int Hq, int Hkv, int S, int window, int sinks) {
   if (!swa_has_far(S, window, sinks)) return 0;
   const int64_t tiles = (int64_t)(Hq / Hkv) * ((S - window + 31) / 32 + 1);
-  const int64_t want = 2 * kSwaCus / ((int64_t)B * Hkv * swa_sink_tiles(S, sinks)), most = (tiles + 7) / 8;
+  const int64_t want = kSwaCus / ((int64_t)B * Hkv * swa_sink_tiles(S, sinks)), most = (tiles + 7) / 8;
   const int64_t n = want < most ? want : most;
   return n < 1 ? 1 : (int)n;
 }
@@ -130,7 +131,7 @@ constexpr int swa_decode_parts(int B, int Hq, int Hkv, int cap, int window, int 
   const int64_t n = want < most ? want : most;
   return n < 1 ? 1 : (int)n;
 }
-// Floats of the decode workspace: none for one part, else [part][B * Hq][D + 2].
+// Floats of the decode workspace: none for one part, else O [part][B * Hq][D], then offset and sum [part][B * Hq][2].
 constexpr int64_t swa_decode_floats(int B, int Hq, int Hkv, int cap, int D, int window, int sinks) {
   const int n = swa_decode_parts(B, Hq, Hkv, cap, window, sinks);
   return n == 1 ? 0 : (int64_t)n * B * Hq * (D + 2);

@@ -22,6 +22,7 @@
 //  * Padded batches: rows from lens[b] on are never read (a tile that reaches
 //    past the end repeats the last row, masked), so they may hold anything;
 //    their O and gradients are 0 and their LSE -inf.
+#include <algorithm>
 #include <utility>
 
 #include "attn_launch.h"
@@ -34,26 +35,41 @@ namespace {
 
 constexpr float kSumMax = 4294967296.0f;  // bound of a block's probability sum before the offset moves
 
-// HBM -> LDS copy of a 32-row tile; rows past `last` repeat row `last`.  The
-// offsets of a thread's chunks are formed at each copy (a minimum and a
-// multiply-add each) from two registers, for any row stride below 2^23.
-template <int D> struct SwaCopy {
-  typedef TileGeom<D> G;
-  static constexpr int N = G::DMA_PER_TENSOR, STEP = 256 / G::CPR;
-  unsigned row, chunk[N];
-  unsigned at;
+// HBM -> LDS copies of pairs of 32-row tiles (K and V, or Q and dO) by a work
+// group of W waves; rows past `last` repeat row `last`.  A wave copies 1 KB
+// pieces: with more waves than a tile has pieces, the first half of them takes
+// one tile and the others the other.  The offsets of a lane's chunks are formed
+// at each copy (a minimum and a multiply-add each), for any row stride below 2^23.
+template <int D, int W> struct SwaCopy {
+  static constexpr int PIECES = TileGeom<D>::TILE / 1024, CPR = TileGeom<D>::CPR;
+  static constexpr bool BOTH = W <= PIECES;  // every wave copies from both tiles
+  static constexpr int N = BOTH ? PIECES / W : 1, STEP = 64 * W / CPR;
+  static constexpr int PER_PAIR = BOTH ? 2 * N : 1;  // copies of each wave
+  static_assert(BOTH || W == 2 * PIECES, "one piece per wave");
+  unsigned row, chunk[N], at;
+  bool second;
   __device__ __forceinline__ void init(int w, int lane) {
-    const int p = w * 64 + lane;
-    row = p / G::CPR;
-    at = w * 64 * 16;
+    second = !BOTH && w >= PIECES;
+    const int p = (BOTH ? w : w % PIECES) * 64 + lane;
+    row = p / CPR;
+    at = (BOTH ? w : w % PIECES) * 1024;
 #pragma unroll
-    for (int i = 0; i < N; ++i) chunk[i] = ((p % G::CPR) ^ swz(row + STEP * i)) << 4;
+    for (int i = 0; i < N; ++i) chunk[i] = ((p % CPR) ^ swz(row + STEP * i)) << 4;
   }
-  __device__ __forceinline__ void copy(const bf16* tile, int rs, int last, char* lds) const {
-    const unsigned dst = lds_addr(lds) + at;
+  __device__ __forceinline__ void one(const bf16* tile, int rs, int last, unsigned lds) const {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      dma16(tile, __umul24(min(row + STEP * i, (unsigned)last), 2u * rs) + chunk[i], dst + i * 256 * 16);
+      dma16(tile, __umul24(min(row + STEP * i, (unsigned)last), 2u * rs) + chunk[i], lds + at + i * W * 1024);
+  }
+  // tile a to lds, tile b behind it
+  __device__ __forceinline__ void pair(const bf16* a, int64_t rsa, const bf16* b, int64_t rsb, int last, char* lds) const {
+    const unsigned dst = lds_addr(lds);
+    if constexpr (BOTH) {
+      one(a, (int)rsa, last, dst);
+      one(b, (int)rsb, last, dst + TileGeom<D>::TILE);
+    } else {
+      one(second ? b : a, (int)(second ? rsb : rsa), last, dst + (second ? TileGeom<D>::TILE : 0));
+    }
   }
 };
 
@@ -110,18 +126,18 @@ __device__ __forceinline__ void contract_trans(const Frags<D>& fr, const char* t
 template <int D> __device__ __forceinline__ int acc_col(int dt, int g, int h) { return dt * 32 + 8 * g + 4 * h; }
 
 // ---------------------------------------------------------------------------
-// Forward.  A work group owns 32 * QG queries of one head (QG = 4 / SPLIT, one
-// wave per 32) and takes its key tiles in SPLIT interleaved parts.
+// Forward.  A work group owns 32 * QG queries of one head and takes its key
+// tiles in SPLIT interleaved parts by W = QG * SPLIT waves.
 // ---------------------------------------------------------------------------
-template <int D, int SPLIT, int NB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT == 1 ? (D == 128 ? 3 : 4) : 1, 10)))
+template <int D, int W, int SPLIT, int NB>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 8 ? 2 : SPLIT > 1 ? 1 : D == 128 ? 3 : 4, 10)))
 void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   typedef TileGeom<D> G;
-  constexpr int QG = 4 / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
-  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_TILE = 2 * G::DMA_PER_TENSOR;
+  constexpr int QG = W / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
+  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_SLOT = SPLIT * SwaCopy<D, W>::PER_PAIR;
   __shared__ __attribute__((aligned(16))) char smem[SPLIT * NB * SET];  // [part][slot][K, V]
-  __shared__ float stats[2][4][SPLIT > 1 ? 64 : 1];
-  static_assert(SPLIT == 1 || 4 * 64 * DT * 16 * 4 <= SPLIT * NB * SET, "merge area");
+  __shared__ float stats[2][W][SPLIT > 1 ? 64 : 1];
+  static_assert(SPLIT == 1 || W * 64 * DT * 16 * 4 <= SPLIT * NB * SET, "merge area");
   static_assert(NB * SET <= 65536, "tile reads reach every slot by immediate offset");
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
@@ -132,15 +148,24 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   const int b = bh / a.Hq, hq = bh - b * a.Hq, hk = hq / (a.Hq / a.Hkv);
   const int len = swa_len(a.lens, b, a.S);
   const int q0 = qt * BQ, qw = q0 + 32 * qg, my_q = qw + r;
-  bf16* orow = (bf16*)a.out + b * a.so.b + hq * a.so.h + my_q * a.so.s;
-  float* lse = a.lse + (int64_t)bh * a.S + my_q;
+  // (pointers from an opaque copy of the row, formed where they are used: kept
+  // from here they would take registers across the loop)
+  auto out_row = [&](int q) {
+    asm volatile("" : "+v"(q));
+    return (bf16*)a.out + b * a.so.b + hq * a.so.h + q * a.so.s;
+  };
+  auto put_lse = [&](int q, float v) {
+    asm volatile("" : "+v"(q));
+    a.lse[(int64_t)bh * a.S + q] = v;
+  };
   auto empty_row = [&] {  // this wave's share of a row without keys
     if (my_q >= a.S || my_q < len) return;
+    bf16* orow = out_row(my_q);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int g = 0; g < 4; ++g) store4<bf16>(orow + acc_col<D>(dt, g, h), 0.f, 0.f, 0.f, 0.f);
-    if (h == 0) *lse = -INFINITY;
+    if (h == 0) put_lse(my_q, -INFINITY);
   };
   if (q0 >= len) {
     if (part == 0) empty_row();
@@ -151,18 +176,17 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   const int L = (kt.n + SPLIT - 1) / SPLIT;
   const bf16* Kb = (const bf16*)a.k + b * a.sk.b + hk * a.sk.h;
   const bf16* Vb = (const bf16*)a.v + b * a.sv.b + hk * a.sv.h;
-  SwaCopy<D> tc;
+  SwaCopy<D, W> tc;
   tc.init(w, lane);
   auto dma = [&](int x, auto slc) {  // iteration x's tile of every part (without one: the last again)
 #pragma unroll
     for (int p = 0; p < SPLIT; ++p) {
       const int row0 = kt.tile(min(x * SPLIT + p, kt.n - 1)) * 32, last = min(31, len - 1 - row0);
       char* dst = smem + (p * NB + decltype(slc)::value) * SET;
-      tc.copy(Kb + row0 * a.sk.s, (int)a.sk.s, last, dst);
-      tc.copy(Vb + row0 * a.sv.s, (int)a.sv.s, last, dst + TILE);
+      tc.pair(Kb + row0 * a.sk.s, a.sk.s, Vb + row0 * a.sv.s, a.sv.s, last, dst);
     }
   };
-  constexpr int GROUP = ring_group(SPLIT, NB, 0, 2);
+  constexpr int GROUP = ring_group(1, NB, 0, 2);
   ring_prologue<NB, GROUP>(L, dma);
   Frags<D> fr;
   fr.init(r, h, lane);
@@ -182,7 +206,7 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
       constexpr int sl = decltype(slc)::value;
       const int i = i0 + sl;
       if (i >= L) return;
-      ring_step<NB, GROUP, 0, SPLIT, PER_TILE, sl>(i, L, dma);
+      ring_step<NB, GROUP, 0, 1, PER_SLOT, sl>(i, L, dma);
       const int x = i * SPLIT + part;
       if (x >= kt.n || qw >= len) return;  // wave-uniform: nothing here, only the barriers
       const int k0 = kt.tile(x) * 32;
@@ -232,6 +256,7 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
     __syncthreads();
     if (part == 0) empty_row();
     if (my_q >= len) return;
+    bf16* orow = out_row(my_q);
     float sp[SPLIT], mn = kMasked;
 #pragma unroll
     for (int p = 0; p < SPLIT; ++p) {
@@ -247,8 +272,8 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
     l = halves_sum(l);
     const float inv = 1.0f / l;
 #pragma unroll
-    for (int gi = 0; gi < QG; ++gi) {
-      const int g = part * QG + gi;
+    for (int gi = 0; gi < 4 / SPLIT; ++gi) {
+      const int g = part * (4 / SPLIT) + gi;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         f32x4 v = get_partial<D>(area, qg, dt, g, lane) * sp[0];
@@ -257,12 +282,13 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
         store4<bf16>(orow + acc_col<D>(dt, g, h), v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
       }
     }
-    if (part == 0 && h == 0) *lse = (mn * c + log2f(l)) * kLn2;
+    if (part == 0 && h == 0) put_lse(my_q, (mn * c + log2f(l)) * kLn2);
     return;
   }
 
   empty_row();
   if (my_q >= len) return;
+  bf16* orow = out_row(my_q);
   const float l = halves_sum(lsum), inv = 1.0f / l;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -270,14 +296,14 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
     for (int g = 0; g < 4; ++g)
       store4<bf16>(orow + acc_col<D>(dt, g, h), oacc[dt][4 * g] * inv, oacc[dt][4 * g + 1] * inv,
                    oacc[dt][4 * g + 2] * inv, oacc[dt][4 * g + 3] * inv);
-  if (h == 0) *lse = (m * c + log2f(l)) * kLn2;
+  if (h == 0) put_lse(my_q, (m * c + log2f(l)) * kLn2);
 }
 
-// The parts' accumulators, added in part order through `area`: f(column, sum of
-// four) for this wave's share of the columns.  Every wave calls it.
-template <int D, int G, typename F>
+// The parts' accumulators of a work group of G row groups (waves grp, grp + G,
+// ... are the SPLIT parts of group grp), added in part order through `area`:
+// f(column, sum of four) for this wave's share of the columns.  Every wave calls it.
+template <int D, int G, int SPLIT, typename F>
 __device__ __forceinline__ void sum_parts(f32x4* area, int w, int h, int lane, const f32x16 (&acc)[D / 32], F&& f) {
-  constexpr int SPLIT = 4 / G;
   if constexpr (SPLIT == 1) {
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
@@ -290,8 +316,8 @@ __device__ __forceinline__ void sum_parts(f32x4* area, int w, int h, int lane, c
     put_partial<D>(area, w, lane, acc);
     __syncthreads();
 #pragma unroll
-    for (int gi = 0; gi < G; ++gi) {
-      const int g = part * G + gi;
+    for (int gi = 0; gi < 4 / SPLIT; ++gi) {
+      const int g = part * (4 / SPLIT) + gi;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
         f32x4 v = get_partial<D>(area, grp, dt, g, lane);
@@ -308,14 +334,14 @@ __device__ __forceinline__ void sum_parts(f32x4* area, int w, int h, int lane, c
 // past the sequence's end) into the workspace for the dK/dV kernels.  The dP
 // contraction starts from D and multiplies by -dO, so it yields D - dP.
 // ---------------------------------------------------------------------------
-template <int D, int SPLIT, int NB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 64 ? 4 : 2, 10)))
+template <int D, int W, int SPLIT, int NB>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 8 ? 2 : SPLIT > 1 ? 1 : D == 64 ? 4 : 2, 10)))
 void swa_dq_bf16_kernel(SwaArgs a, float c) {
   typedef TileGeom<D> G;
-  constexpr int QG = 4 / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
-  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_TILE = 2 * G::DMA_PER_TENSOR;
+  constexpr int QG = W / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
+  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_SLOT = SPLIT * SwaCopy<D, W>::PER_PAIR;
   __shared__ __attribute__((aligned(16))) char smem[SPLIT * NB * SET];  // [part][slot][K, V]
-  static_assert(SPLIT == 1 || 4 * 64 * DT * 16 * 4 <= SPLIT * NB * SET, "merge area");
+  static_assert(SPLIT == 1 || W * 64 * DT * 16 * 4 <= SPLIT * NB * SET, "merge area");
   static_assert(NB * SET <= 65536, "tile reads reach every slot by immediate offset");
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
@@ -326,9 +352,15 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
   const int b = bh / a.Hq, hq = bh - b * a.Hq, hk = hq / (a.Hq / a.Hkv);
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int q0 = qt * BQ, qw = q0 + 32 * qg, my_q = qw + r;
-  bf16* row = (bf16*)a.dq + b * a.sdq.b + hq * a.sdq.h + my_q * a.sdq.s;
   float* wsh = a.ws + (int64_t)bh * 2 * Sp;
+  // (from an opaque copy of the row: kept from here, a pointer would take two
+  // registers across the loop)
+  auto out_row = [&](int q) {
+    asm volatile("" : "+v"(q));
+    return (bf16*)a.dq + b * a.sdq.b + hq * a.sdq.h + q * a.sdq.s;
+  };
   if (q0 >= len) {  // (no work group reads this one's workspace rows)
+    bf16* row = out_row(my_q);
     if (part == 0 && my_q < a.S)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -341,18 +373,17 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
   const int L = (kt.n + SPLIT - 1) / SPLIT;
   const bf16* Kb = (const bf16*)a.k + b * a.sk.b + hk * a.sk.h;
   const bf16* Vb = (const bf16*)a.v + b * a.sv.b + hk * a.sv.h;
-  SwaCopy<D> tc;
+  SwaCopy<D, W> tc;
   tc.init(w, lane);
   auto dma = [&](int x, auto slc) {
 #pragma unroll
     for (int p = 0; p < SPLIT; ++p) {
       const int row0 = kt.tile(min(x * SPLIT + p, kt.n - 1)) * 32, last = min(31, len - 1 - row0);
       char* dst = smem + (p * NB + decltype(slc)::value) * SET;
-      tc.copy(Kb + row0 * a.sk.s, (int)a.sk.s, last, dst);
-      tc.copy(Vb + row0 * a.sv.s, (int)a.sv.s, last, dst + TILE);
+      tc.pair(Kb + row0 * a.sk.s, a.sk.s, Vb + row0 * a.sv.s, a.sv.s, last, dst);
     }
   };
-  constexpr int GROUP = ring_group(SPLIT, NB, 0, 2);
+  constexpr int GROUP = ring_group(1, NB, 0, 2);
   ring_prologue<NB, GROUP>(L, dma);
   Frags<D> fr;
   fr.init(r, h, lane);
@@ -389,7 +420,7 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
       constexpr int sl = decltype(slc)::value;
       const int i = i0 + sl;
       if (i >= L) return;
-      ring_step<NB, GROUP, 0, SPLIT, PER_TILE, sl>(i, L, dma);
+      ring_step<NB, GROUP, 0, 1, PER_SLOT, sl>(i, L, dma);
       const int x = i * SPLIT + part;
       if (x >= kt.n || qw >= len) return;
       const int k0 = kt.tile(x) * 32;
@@ -426,7 +457,8 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
   }
 
   if constexpr (SPLIT > 1) wait_vm(0);  // the rings' last copies
-  sum_parts<D, QG>((f32x4*)smem, w, h, lane, acc, [&](int col, const f32x4& v) {
+  bf16* row = out_row(my_q);
+  sum_parts<D, QG, SPLIT>((f32x4*)smem, w, h, lane, acc, [&](int col, const f32x4& v) {
     if (my_q < len) store4<bf16>(row + col, v[0] * a.scale, v[1] * a.scale, v[2] * a.scale, v[3] * a.scale);
     else if (my_q < a.S) store4<bf16>(row + col, 0.f, 0.f, 0.f, 0.f);
   });
@@ -435,22 +467,23 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
 // ---------------------------------------------------------------------------
 // Backward, kernel 2: dK, dV.  A work group owns 32 * KG keys of one key/value
 // head and walks, for each query head of the group, the query tiles that see
-// them from the last down, in SPLIT interleaved parts.  FAR: the pairs that
+// them from the last down, in SPLIT interleaved parts by W = KG * SPLIT waves.  FAR: the pairs that
 // only the sinks see, 32 sink keys and one part of the walk a work group, into
 // the far area; otherwise the pairs of the window.
 // ---------------------------------------------------------------------------
-template <int D, int SPLIT, int NB, bool FAR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 64 ? 3 : 2, 10)))
+template <int D, int W, int SPLIT, int NB, bool FAR>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 8 ? 2 : SPLIT > 1 ? 1 : D == 64 ? 3 : 2, 10)))
 void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   typedef TileGeom<D> G;
-  constexpr int KG = 4 / SPLIT, BKV = 32 * KG, KS_D = D / 16, DT = D / 32;
+  constexpr int KG = W / SPLIT, BKV = 32 * KG, KS_D = D / 16, DT = D / 32;
   constexpr int TILE = G::TILE, SETB = 2 * TILE, AUX = 2 * 32 * 4, AUX0 = SPLIT * NB * SETB;
-  constexpr int PER_TILE = 2 * G::DMA_PER_TENSOR + 1;
+  constexpr int AUX_COPIES = 4 * SPLIT / W, PER_SLOT = SPLIT * SwaCopy<D, W>::PER_PAIR + AUX_COPIES;
+  static_assert(AUX_COPIES * W == 4 * SPLIT, "four waves copy a part's workspace rows");
   // [part][slot] Q, dO tiles, then [part][slot] -LSE/scale and D rows
   __shared__ __attribute__((aligned(16))) char smem[SPLIT * NB * (SETB + AUX)];
-  static_assert(SPLIT == 1 || 4 * 64 * DT * 16 * 4 <= SPLIT * NB * SETB, "merge area");
+  static_assert(SPLIT == 1 || W * 64 * DT * 16 * 4 <= SPLIT * NB * SETB, "merge area");
   static_assert(NB * SETB <= 65536, "tile reads reach every slot by immediate offset");
-  static_assert(!FAR || SPLIT == 4, "a tile of sinks is one key group");
+  static_assert(!FAR || KG == 1, "a tile of sinks is one key group");
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -462,8 +495,6 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int k0 = kt * BKV, kw = k0 + 32 * kg, my_k = kw + r;
   const bool far = FAR || swa_has_far(a.S, a.window, a.sinks);  // sink keys' sums go to the far area
-  bf16* krow = (bf16*)a.dk + b * a.sdk.b + hk * a.sdk.h + my_k * a.sdk.s;
-  bf16* vrow = (bf16*)a.dv + b * a.sdv.b + hk * a.sdv.h + my_k * a.sdv.s;
 
   // query tiles jlo .. jhi of every head of the group see a key of this work group
   const int jlo = FAR ? (k0 + a.window) / 32 : k0 / 32;
@@ -477,13 +508,13 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   }
   const int L = (n + SPLIT - 1) / SPLIT;
 
-  SwaCopy<D> tc;
+  SwaCopy<D, W> tc;
   tc.init(w, lane);
   const bf16* Qb = (const bf16*)a.q + b * a.sq.b + (int64_t)hk * group * a.sq.h;
   const bf16* dOb = (const bf16*)a.dout + b * a.sdo.b + (int64_t)hk * group * a.sdo.h;
   const float* wsb = a.ws + ((int64_t)b * a.Hq + hk * group) * 2 * Sp;
-  // lanes 0..3 of every wave copy the 8 chunks of -LSE/scale, then the 8 of D
-  const int ldq = 4 * w + (lane & 3);
+  // a part's 8 chunks of -LSE/scale and 8 of D: lanes 0..3 of four waves
+  const int ldq = 4 * (w & 3) + (lane & 3);
   const unsigned ld_voff = (unsigned)((ldq < 8 ? Sp + 4 * ldq : 4 * (ldq - 8)) * 4);
   // the walk: position x is query tile jhi - x % nj of head x / nj
   int head = n ? x0 / nj : 0, j = n ? jhi - x0 % nj : 0;  // next position to copy
@@ -493,11 +524,10 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
     for (int p = 0; p < SPLIT; ++p) {
       const int row0 = j * 32, last = min(31, len - 1 - row0);
       char* dst = smem + (p * NB + decltype(slc)::value) * SETB;
-      tc.copy(Qb + head * a.sq.h + row0 * a.sq.s, (int)a.sq.s, last, dst);
-      tc.copy(dOb + head * a.sdo.h + row0 * a.sdo.s, (int)a.sdo.s, last, dst + TILE);
-      if (lane < 4)
+      tc.pair(Qb + head * a.sq.h + row0 * a.sq.s, a.sq.s, dOb + head * a.sdo.h + row0 * a.sdo.s, a.sdo.s, last, dst);
+      if ((W == 4 || w / 4 == p) && lane < 4)
         dma16(wsb + (int64_t)head * 2 * Sp + row0, ld_voff,
-              lds_addr(smem + AUX0 + (p * NB + decltype(slc)::value) * AUX) + 64 * w);
+              lds_addr(smem + AUX0 + (p * NB + decltype(slc)::value) * AUX) + 64 * (w & 3));
       if (x * SPLIT + p + 1 < n && --j < jlo) {  // (a part without a tile copies the last again)
         j = jhi;
         ++head;
@@ -508,7 +538,7 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
     at -= by;
     while (at < jlo) at += nj;
   };
-  constexpr int GROUP = ring_group(SPLIT, NB, 0, 2);
+  constexpr int GROUP = ring_group(1, NB, 0, 2);
   ring_prologue<NB, GROUP>(L, dma);
   if (n) advance(jc, part);
   Frags<D> fr;
@@ -535,7 +565,7 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
       constexpr int sl = decltype(slc)::value;
       const int i = i0 + sl;
       if (i >= L) return;
-      ring_step<NB, GROUP, 0, SPLIT, PER_TILE, sl>(i, L, dma);
+      ring_step<NB, GROUP, 0, 1, PER_SLOT, sl>(i, L, dma);
       if (i * SPLIT + part >= n) return;
       const int qs = jc * 32;
       advance(jc, SPLIT);
@@ -605,105 +635,137 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
 
   if constexpr (SPLIT > 1) wait_vm(0);
   const int dim = D;
+  int key = my_k;
+  asm volatile("" : "+v"(key));  // (no pointers kept across the loop)
+  bf16* krow = (bf16*)a.dk + b * a.sdk.b + hk * a.sdk.h + key * a.sdk.s;
+  bf16* vrow = (bf16*)a.dv + b * a.sdv.b + hk * a.sdv.h + key * a.sdv.s;
   auto put = [&](bf16* out, int which, float f, int col, const f32x4& v) {
     if (FAR || (far && my_k < a.sinks && my_k < len)) {
-      *(f32x4*)(swa_far_slot(a, bkv, my_k, FAR ? 1 + chunk : 0, far_parts) + which * 32 * dim + col) = v;
+      if (!FAR || my_k < a.sinks) *(f32x4*)(swa_far_slot(a, bkv, my_k, FAR ? 1 + chunk : 0, far_parts) + which * 32 * dim + col) = v;
     } else if (my_k < len) {
       store4<bf16>(out + col, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
     } else if (my_k < a.S) {
       store4<bf16>(out + col, 0.f, 0.f, 0.f, 0.f);
     }
   };
-  sum_parts<D, KG>((f32x4*)smem, w, h, lane, dkacc, [&](int col, const f32x4& v) { put(krow, 0, a.scale, col, v); });
-  sum_parts<D, KG>((f32x4*)smem, w, h, lane, dvacc, [&](int col, const f32x4& v) { put(vrow, 1, 1.f, col, v); });
+  sum_parts<D, KG, SPLIT>((f32x4*)smem, w, h, lane, dkacc, [&](int col, const f32x4& v) { put(krow, 0, a.scale, col, v); });
+  sum_parts<D, KG, SPLIT>((f32x4*)smem, w, h, lane, dvacc, [&](int col, const f32x4& v) { put(vrow, 1, 1.f, col, v); });
 }
 
-// dK, dV of the sink keys: the window's sum, then the far parts', in order.
+// dK (blockIdx.y = 0) and dV (1) of one sink key: the window's sum and the far
+// parts'.  A thread takes four columns of every n-th partial row, n = 256 / (D /
+// 4); the n sums meet in LDS and are added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void swa_far_sum_kernel(SwaArgs a, int far_parts) {
-  const int tiles = swa_sink_tiles(a.S, a.sinks);
-  const int bkv = blockIdx.x / tiles, tile = blockIdx.x - bkv * tiles;
-  const int b = bkv / a.Hkv, hk = bkv - b * a.Hkv, len = swa_len(a.lens, b, a.S);
-  const int quads = a.D / 4;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < 2 * 32 * quads; i += gridDim.y * 256) {
-    const int which = i / (32 * quads), rem = i - which * 32 * quads, row = rem / quads, col = (rem - row * quads) * 4;
-    const int key = tile * 32 + row;
-    if (key >= a.sinks || key >= len) continue;
-    const float* p = swa_far_slot(a, bkv, key, 0, far_parts) + which * 32 * a.D + col;
-    f32x4 v = *(const f32x4*)p;
-    for (int s = 1; s <= far_parts; ++s) v += *(const f32x4*)(p + (int64_t)s * 2 * 32 * a.D);
-    const Strides& st = which ? a.sdv : a.sdk;
-    T* out = (T*)(which ? a.dv : a.dk) + b * st.b + hk * st.h + key * st.s + col;
-    const float f = which ? 1.f : a.scale;
-    if constexpr (sizeof(T) == 2) store4<bf16>(out, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-    else *(f32x4*)out = v * f;
-  }
+  __shared__ f32x4 sums[256];
+  const int n_sinks = min(a.sinks, a.S);
+  const int bkv = blockIdx.x / n_sinks, key = blockIdx.x - bkv * n_sinks, which = blockIdx.y;
+  const int b = bkv / a.Hkv, hk = bkv - b * a.Hkv;
+  if (key >= swa_len(a.lens, b, a.S)) return;
+  const int quads = a.D / 4, n = 256 / quads, q = threadIdx.x % quads, s0 = threadIdx.x / quads;
+  const f32x4* p = (const f32x4*)(swa_far_slot(a, bkv, key, 0, far_parts) + which * 32 * a.D) + q;
+  f32x4 v{};
+#pragma unroll 4
+  for (int s = s0; s <= far_parts; s += n) v += p[(int64_t)s * 2 * 32 * quads];
+  sums[threadIdx.x] = v;
+  __syncthreads();
+  if (s0) return;
+  for (int i = 1; i < n; ++i) v += sums[i * quads + q];
+  const Strides& st = which ? a.sdv : a.sdk;
+  T* out = (T*)(which ? a.dv : a.dk) + b * st.b + hk * st.h + key * st.s + 4 * q;
+  const float f = which ? 1.f : a.scale;
+  if constexpr (sizeof(T) == 2) store4<bf16>(out, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+  else *(f32x4*)out = v * f;
 }
 
 // ---------------------------------------------------------------------------
 // Launchers
 // ---------------------------------------------------------------------------
-template <int SPLIT, typename F> hipError_t launch_rows(F kernel, const SwaArgs& a, int heads, hipStream_t st) {
-  constexpr int ROWS = 128 / SPLIT;
-  const unsigned grid = (unsigned)((int64_t)a.B * heads * ((a.S + ROWS - 1) / ROWS));
-  kernel(dim3(grid), a.scale * kLog2e, st);
+// Work groups of ROWS rows of each of `heads` heads a sequence.
+template <int ROWS> dim3 rows_grid(const SwaArgs& a, int heads) {
+  return dim3((unsigned)((int64_t)a.B * heads * ((a.S + ROWS - 1) / ROWS)));
+}
+
+// How a kernel's work groups divide their walk over the other axis: not (128
+// rows, four waves), in two parts (64 rows), in four (32 rows), or in two parts by
+// eight waves (128 rows).  A grid of few 128-row work groups leaves CUs idle and
+// its waves the whole walk; more parts cost rings, LDS and the parts' merge.  What
+// decides are the 32-row groups per CU, g, and `run`, the tiles a work group walks
+// (of all heads of the group in dK/dV).  Measured, none / two / four parts / eight
+// waves, us (MHA unless Hq/Hkv; F forward, Q dQ, K dK/dV with the other kernel's
+// time in; S, window):
+//   D  64  g 1    F 15.5 / 10.5 / 9.0 (1024, 512), K 180 / 144 / 123 (8192, 4096)
+//          g 2    F 9.7 / 8.7 / 8.8, K 23.0 / 20.2 / 20.7 (1024, 128); F 15.5 / 10.7 / 9.9, K 38.3 / 32.2 / 30.7
+//                 (1024, 512); K 8/2 267 / 188 / 176 (8192, 2048)
+//          g 4    F 15.9 / 12.8 / 16.7, K 39.1 / 36.0 / 40.8 (1024, 512); K 16/4 183 / 161 / 185 (8192, 1024)
+//          g 6    F 12.0 / 13.6, K 30.5 / 32.5 (1024, 128); F 69.1 / 71.8, K 190 / 199 (8192, 4096)
+//   D 128  g 1    F 22.0 / 13.5 / 11.4, K 55.7 / 45.1 / 40.7 (1024, 512)
+//          g 2    F 14.0 / 9.6 / 15.3, K 33.2 / 28.3 / 35.6 (1024, 128); K 8/2 424 / 288 / 341 / 357 (8192, 2048)
+//          g 4    F 14.8 / 12.2, Q 37.0 / 38.0, K 36.8 / 42.5 / - / 38.8 (1024, 128); F 22.6 / 17.4, Q 58.5 / 56.8, K
+//                 58.2 / 65.3 / - / 57.1 (1024, 512); K 16/4 293 / 313 / - / 264 (8192, 1024)
+//          g 6    F 19.9 / 19.3 (1024, 128), 109 / 117 (8192, 4096); Q 319 / 341, K 321 / 364 / - / 345 (8192, 4096)
+enum Form { kWhole = 1, kTwo = 2, kFour = 4, kEight = 8 };
+Form form_of(Pass pass, int D, int64_t heads, int S, int run) {
+  const int64_t groups = heads * ((S + 31) / 32), cus = cu_count();
+  if (groups <= cus || (D == 64 && groups <= 2 * cus && run >= 16)) return kFour;
+  if (groups > 4 * cus) return kWhole;
+  if (D == 64 || pass == Pass::kFwd || groups <= 2 * cus) return kTwo;
+  if (run < 16) return kWhole;
+  return pass == Pass::kDq ? kTwo : kEight;
+}
+// Tiles that a work group of 128 rows walks on one head.
+int run_of(const SwaArgs& a) {
+  return std::min((a.S + 31) / 32, (std::min(a.window, a.S) + 127) / 32 + swa_sink_tiles(a.S, a.sinks));
+}
+
+template <int D, int W, int SPLIT, int NB> hipError_t fwd_s(const SwaArgs& a, float c, hipStream_t st) {
+  hipLaunchKernelGGL((swa_fwd_bf16_kernel<D, W, SPLIT, NB>), rows_grid<32 * W / SPLIT>(a, a.Hq), dim3(64 * W), 0, st, a,
+                     c);
   return hipGetLastError();
 }
-
-// Parts that a work group's waves split the other axis into.
-int parts_of(int heads, int S) {
-  const int64_t n128 = (int64_t)heads * ((S + 127) / 128), cus = cu_count();
-  return n128 >= 2 * cus ? 1 : n128 >= cus ? 2 : 4;
+template <int D, int W, int SPLIT, int NB> hipError_t dq_s(const SwaArgs& a, float c, hipStream_t st) {
+  hipLaunchKernelGGL((swa_dq_bf16_kernel<D, W, SPLIT, NB>), rows_grid<32 * W / SPLIT>(a, a.Hq), dim3(64 * W), 0, st, a,
+                     c);
+  return hipGetLastError();
 }
-
-template <int D, int SPLIT> hipError_t fwd_s(const SwaArgs& a, hipStream_t st) {
-  constexpr int NB = SPLIT > 1 ? 2 : D == 64 ? 4 : 3;
-  return launch_rows<SPLIT>([&](dim3 grid, float c, hipStream_t s) {
-    hipLaunchKernelGGL((swa_fwd_bf16_kernel<D, SPLIT, NB>), grid, dim3(256), 0, s, a, c);
-  }, a, a.Hq, st);
-}
-template <int D, int SPLIT> hipError_t dq_s(const SwaArgs& a, hipStream_t st) {
-  constexpr int NB = SPLIT > 1 ? 2 : 4;
-  return launch_rows<SPLIT>([&](dim3 grid, float c, hipStream_t s) {
-    hipLaunchKernelGGL((swa_dq_bf16_kernel<D, SPLIT, NB>), grid, dim3(256), 0, s, a, c);
-  }, a, a.Hq, st);
-}
-template <int D, int SPLIT> hipError_t dkdv_s(const SwaArgs& a, hipStream_t st) {
-  constexpr int NB = SPLIT > 1 ? 2 : 4;
-  const int far = swa_far_parts(a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
-  return launch_rows<SPLIT>([&](dim3 grid, float c, hipStream_t s) {
-    hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, SPLIT, NB, false>), grid, dim3(256), 0, s, a, c, far);
-  }, a, a.Hkv, st);
-}
-template <int D> hipError_t far_d(const SwaArgs& a, hipStream_t st) {
-  const int far = swa_far_parts(a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
-  const unsigned grid = (unsigned)((int64_t)a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks) * far);
-  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 2, true>), dim3(grid), dim3(256), 0, st, a, a.scale * kLog2e, far);
+template <int D, int W, int SPLIT, int NB> hipError_t dkdv_s(const SwaArgs& a, float c, int far, hipStream_t st) {
+  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, W, SPLIT, NB, false>), rows_grid<32 * W / SPLIT>(a, a.Hkv), dim3(64 * W), 0,
+                     st, a, c, far);
   return hipGetLastError();
 }
 
 template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
-  switch (parts_of(a.B * a.Hq, a.S)) {
-    case 4: return fwd_s<D, 4>(a, st);
-    case 2: return fwd_s<D, 2>(a, st);
-    default: return fwd_s<D, 1>(a, st);
+  const float c = a.scale * kLog2e;
+  switch (form_of(Pass::kFwd, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
+    case kFour: return fwd_s<D, 4, 4, 2>(a, c, st);
+    case kTwo: return fwd_s<D, 4, 2, D == 64 ? 4 : 2>(a, c, st);
+    default: return fwd_s<D, 4, 1, D == 64 ? 4 : 3>(a, c, st);
   }
 }
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
+  const float c = a.scale * kLog2e;
+  const int far = swa_far_parts(a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
   hipError_t e;
-  switch (parts_of(a.B * a.Hq, a.S)) {
-    case 4: e = dq_s<D, 4>(a, st); break;
-    case 2: e = dq_s<D, 2>(a, st); break;
-    default: e = dq_s<D, 1>(a, st);
+  switch (form_of(Pass::kDq, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
+    case kFour: e = dq_s<D, 4, 4, 2>(a, c, st); break;
+    case kTwo: e = dq_s<D, 4, 2, D == 64 ? 4 : 2>(a, c, st); break;
+    default: e = dq_s<D, 4, 1, 4>(a, c, st);
   }
   if (e != hipSuccess) return e;
-  switch (parts_of(a.B * a.Hkv, a.S)) {
-    case 4: e = dkdv_s<D, 4>(a, st); break;
-    case 2: e = dkdv_s<D, 2>(a, st); break;
-    default: e = dkdv_s<D, 1>(a, st);
+  switch (form_of(Pass::kDkdv, D, (int64_t)a.B * a.Hkv, a.S, run_of(a) * (a.Hq / a.Hkv))) {
+    case kFour: e = dkdv_s<D, 4, 4, 2>(a, c, far, st); break;
+    case kTwo: e = dkdv_s<D, 4, 2, D == 64 ? 4 : 2>(a, c, far, st); break;
+    case kEight:
+      if constexpr (D == 128) {
+        e = dkdv_s<D, 8, 2, 4>(a, c, far, st);
+        break;
+      }
+    default: e = dkdv_s<D, 4, 1, 4>(a, c, far, st);
   }
-  if (e != hipSuccess || !swa_has_far(a.S, a.window, a.sinks)) return e;
-  e = far_d<D>(a, st);
+  if (e != hipSuccess || !far) return e;
+  const unsigned grid = (unsigned)((int64_t)a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks) * far);
+  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 4, 2, true>), dim3(grid), dim3(256), 0, st, a, c, far);
+  e = hipGetLastError();
   return e != hipSuccess ? e : launch_swa_far_sum(a, st);
 }
 
@@ -711,7 +773,7 @@ template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
 
 hipError_t launch_swa_far_sum(const SwaArgs& a, hipStream_t st) {
   const int far = swa_far_parts(a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
-  const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks)), (unsigned)(a.D * 64 / 4 / 256));
+  const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * (a.sinks < a.S ? a.sinks : a.S)), 2);
   if (a.bf16) hipLaunchKernelGGL((swa_far_sum_kernel<bf16>), grid, dim3(256), 0, st, a, far);
   else hipLaunchKernelGGL((swa_far_sum_kernel<float>), grid, dim3(256), 0, st, a, far);
   return hipGetLastError();

@@ -324,7 +324,8 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
 
   auto put = [&](float* out, int which, float f, int g, const ColBlocks<D>& v) {
     if (FAR || (far && my_k < a.sinks && my_k < len)) {
-      store_cols<D>(swa_far_slot(a, bkv, my_k, FAR ? 1 + chunk : 0, far_parts) + which * 32 * D, g, h, v, 1.f);
+      if (!FAR || my_k < a.sinks)
+        store_cols<D>(swa_far_slot(a, bkv, my_k, FAR ? 1 + chunk : 0, far_parts) + which * 32 * D, g, h, v, 1.f);
     } else if (my_k < a.S) {
       if (my_k < len) store_cols<D>(out, g, h, v, f);
       else store_cols<D>(out, g, h, ColBlocks<D>{}, 0.f);
