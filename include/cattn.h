@@ -387,7 +387,7 @@ cattn_status cattn_rope_frequencies(double* freqs, int rot, double base, int sca
  *             strides): rotated in place.
  *   positions: int32 [B, S] (batched != 0) or [S], or NULL: 0 .. S - 1
  *   freqs:    DEVICE double [rot / 2]
- * Supported: D even, 2 .. 512; rot even, 2 .. D; B * S < 2^31.  Any strides and
+ * Supported: D even, 2 .. 512; rot even, 2 .. D; B * S < 2^31 - 1.  Any strides and
  * element-aligned addresses; 16-byte ones with rot / 2 (interleaved: rot) and
  * D - rot multiples of 16 bytes are the fast path.
  */

@@ -16,16 +16,11 @@ from typing import Optional
 
 import torch
 
-from .binding import (CATTN_OK, CattnError, _check_workspace, _dtype_code, _LAYOUTS, _ptr, _rows_cols, _stream,
+from .binding import (CATTN_OK, CattnError, _check_workspace, _dtype_code, _LAYOUTS, _rows_cols, _stream,
                       last_error_string, lib)
 
 _F32, _F64, _I32 = torch.float32, torch.float64, torch.int32
 _SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
-
-
-def _done(status: int, where: str):
-    if status != CATTN_OK:
-        raise CattnError(status, where, last_error_string())
 
 
 # One expression decides; only then is it looked for what is wrong (binding.py).
@@ -47,6 +42,11 @@ def _view(name, t, shape, dtype, device):
     raise ValueError(f"the last dimension of {name} must be consecutive")
 
 
+def _rows_consecutive(name, t):
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError(f"the last dimension of {name} must be consecutive")
+
+
 def _refuse(name, t, shape, dtype, device):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -65,22 +65,32 @@ def _on_hip(name, t):
         raise ValueError(f"{name} must live on a HIP device")
 
 
-class _current:
-    """Makes the tensors' device the current one for the call, where it is not."""
+_get_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
-    __slots__ = ("index", "was")
 
-    def __init__(self, device):
-        self.index = device.index
+def _run(where: str, device, *args):
+    """Calls the library's `where` on torch's current stream of the tensors' device, which is made
+    the current one for the call if it is not."""
+    was = _get_device()
+    if was == device.index:
+        st = getattr(lib(), where)(*args, _stream(device))
+    else:
+        torch.cuda.set_device(device)
+        try:
+            st = getattr(lib(), where)(*args, _stream(device))
+        finally:
+            torch.cuda.set_device(was)
+    if st != CATTN_OK:
+        raise CattnError(st, where, last_error_string())
 
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.index != self.was:
-            torch.cuda.set_device(self.index)
 
-    def __exit__(self, *_):
-        if self.index != self.was:
-            torch.cuda.set_device(self.was)
+def _at(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _int(n) -> int:
+    """n as a C int: what does not fit becomes the largest (or -1), which the library clamps or refuses."""
+    return n if -1 <= n <= 2147483647 else 2147483647 if n > 0 else -1
 
 
 def _heads(name, t, layout):
@@ -126,15 +136,17 @@ def _batch(name, t, B, device):
 # ---------------------------------------------------------------------------
 # RMSNorm
 # ---------------------------------------------------------------------------
+# (new_empty and empty_like cost less host time than torch.empty with its keywords)
 def _norm_inputs(x, gamma, residual):
     _on_hip("x", x)
     R, C = _rows_cols(x)
-    _plain("x", x, x.shape, x.dtype, x.device)
+    if not x.is_contiguous():
+        raise ValueError("x must be contiguous")
     _plain("gamma", gamma, (C,), _F32, x.device)
-    if residual is not None:
-        _plain("residual", residual, x.shape, x.dtype, x.device)
-    return R, C, torch.empty_like(x) if residual is not None else None, \
-        torch.empty((R,), dtype=_F32, device=x.device)
+    if residual is None:
+        return R, C, None, gamma.new_empty(R), _dtype_code(x)
+    _plain("residual", residual, x.shape, x.dtype, x.device)
+    return R, C, torch.empty_like(x), gamma.new_empty(R), _dtype_code(x)
 
 
 def rmsnorm_fwd(x, gamma, residual=None, eps: float = 1e-5):
@@ -143,13 +155,10 @@ def rmsnorm_fwd(x, gamma, residual=None, eps: float = 1e-5):
     x (and residual): float32 or bfloat16, contiguous; gamma: float32 [C].  h is
     x itself without a residual; rstd is float32 [rows].
     """
-    R, C, h, rstd = _norm_inputs(x, gamma, residual)
-    code = _dtype_code(x)
+    R, C, h, rstd, code = _norm_inputs(x, gamma, residual)
     y = torch.empty_like(x)
-    with _current(x.device):
-        st = lib().cattn_rmsnorm_fwd(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(y), _ptr(h), _ptr(rstd), R, C,
-                                     float(eps), code, _stream(x.device))
-    _done(st, "cattn_rmsnorm_fwd")
+    _run("cattn_rmsnorm_fwd", x.device, _at(x), _at(residual), _at(gamma), _at(y), _at(h), _at(rstd), _int(R), C, eps,
+         code)
     return y, x if h is None else h, rstd
 
 
@@ -159,16 +168,13 @@ def rmsnorm_fwd_q8(x, gamma, residual=None, eps: float = 1e-5, group: int = 0):
     q is float8_e4m3fn of x's shape; scale float32 [rows, ceil(C / group)], one per
     `group` consecutive columns (a power of two from 8 to 512), or one per row for 0.
     """
-    R, C, h, rstd = _norm_inputs(x, gamma, residual)
-    code = _dtype_code(x)
+    R, C, h, rstd, code = _norm_inputs(x, gamma, residual)
     if not isinstance(group, int) or (group and (group < 8 or group > 512 or group & (group - 1))):
         raise ValueError("group must be 0 or a power of two from 8 to 512")
-    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-    scale = torch.empty((R, -(-C // group) if group else 1), dtype=_F32, device=x.device)
-    with _current(x.device):
-        st = lib().cattn_rmsnorm_fwd_q8(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(q), _ptr(scale), _ptr(h),
-                                        _ptr(rstd), R, C, group, float(eps), code, _stream(x.device))
-    _done(st, "cattn_rmsnorm_fwd_q8")
+    q = torch.empty_like(x, dtype=torch.float8_e4m3fn)
+    scale = gamma.new_empty((R, -(-C // group) if group else 1))
+    _run("cattn_rmsnorm_fwd_q8", x.device, _at(x), _at(residual), _at(gamma), _at(q), _at(scale), _at(h), _at(rstd),
+         _int(R), C, group, eps, code)
     return q, scale, x if h is None else h, rstd
 
 
@@ -185,23 +191,22 @@ def rmsnorm_bwd(h, gamma, rstd, dy, dh=None, workspace=None):
     _on_hip("h", h)
     R, C = _rows_cols(h)
     code = _dtype_code(h)
-    _plain("h", h, h.shape, h.dtype, h.device)
+    if not h.is_contiguous():
+        raise ValueError("h must be contiguous")
     _plain("gamma", gamma, (C,), _F32, h.device)
     _plain("rstd", rstd, (R,), _F32, h.device)
     _plain("dy", dy, h.shape, h.dtype, h.device)
     if dh is not None:
         _plain("dh", dh, h.shape, h.dtype, h.device)
     dx = torch.empty_like(h)
-    dgamma = torch.empty((C,), dtype=_F32, device=h.device) if R else torch.zeros((C,), dtype=_F32, device=h.device)
+    dgamma = torch.empty_like(gamma) if R else torch.zeros_like(gamma)  # (no rows: a sum over nothing)
     n = rmsnorm_bwd_workspace_bytes(R, C) // 4
     if workspace is None:
-        workspace = torch.empty((n,), dtype=_F32, device=h.device)
+        workspace = gamma.new_empty(n)
     else:
         _check_workspace(workspace, n, h.device)
-    with _current(h.device):
-        st = lib().cattn_rmsnorm_bwd(_ptr(h), _ptr(gamma), _ptr(rstd), _ptr(dy), _ptr(dh), _ptr(dx), _ptr(dgamma),
-                                     _ptr(workspace), R, C, code, _stream(h.device))
-    _done(st, "cattn_rmsnorm_bwd")
+    _run("cattn_rmsnorm_bwd", h.device, _at(h), _at(gamma), _at(rstd), _at(dy), _at(dh), _at(dx), _at(dgamma),
+         _at(workspace), _int(R), C, code)
     return dx, dgamma
 
 
@@ -220,8 +225,9 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", fac
         raise ValueError(f"scaling must be one of {sorted(_SCALINGS)}, not {scaling!r}")
     rot = int(rot)
     out = (ctypes.c_double * max(1, rot // 2))()
-    _done(lib().cattn_rope_frequencies(out, rot, float(base), _SCALINGS[scaling], float(factor), float(context),
-                                       float(low), float(high)), "cattn_rope_frequencies")
+    st = lib().cattn_rope_frequencies(out, rot, base, _SCALINGS[scaling], factor, context, low, high)
+    if st != CATTN_OK:
+        raise CattnError(st, "cattn_rope_frequencies", last_error_string())
     return torch.tensor(list(out), dtype=_F64, device=device)
 
 
@@ -229,7 +235,7 @@ def _rope(q, k, freqs, positions, layout, interleaved, amplitude, q_out, k_out, 
     B, Hq, S, D = _heads("q", q, layout)
     code = _dtype_code(q)
     dev = q.device
-    _view("q", q, q.shape, q.dtype, dev)
+    _rows_consecutive("q", q)
     Hkv = 0
     if k is not None:
         Hkv = _heads("k", k, layout)[1]
@@ -244,20 +250,17 @@ def _rope(q, k, freqs, positions, layout, interleaved, amplitude, q_out, k_out, 
         batched = int(isinstance(positions, torch.Tensor) and positions.dim() == 2)
         _plain("positions", positions, (B, S) if batched else (S,), _I32, dev)
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        q_out = q.new_empty(q.shape)
     else:
         _view("q_out", q_out, q.shape, q.dtype, dev)
     if k is not None:
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=q.dtype, device=dev)
+            k_out = k.new_empty(k.shape)
         else:
             _view("k_out", k_out, k.shape, q.dtype, dev)
     strides = _strides((q, k, q_out, k_out) if k is not None else (q, q, q_out, q_out), layout)
-    with _current(dev):
-        st = lib().cattn_rope(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _ptr(positions), _ptr(freqs), B, S, Hq, Hkv,
-                              D, 2 * freqs.shape[0], batched, strides, _LAYOUTS[layout], int(bool(interleaved)),
-                              inverse, float(amplitude), code, _stream(dev))
-    _done(st, "cattn_rope")
+    _run("cattn_rope", dev, _at(q), _at(k), _at(q_out), _at(k_out), _at(positions), _at(freqs), _int(B), _int(S), Hq,
+         Hkv, D, 2 * freqs.shape[0], batched, strides, _LAYOUTS[layout], bool(interleaved), inverse, amplitude, code)
     return q_out, k_out
 
 
@@ -294,7 +297,7 @@ def rope_append(q, k, v, k_cache, v_cache, lens, freqs, counts=None, window: int
     dev, dt = q.device, q.dtype
     Hkv = _heads("k", k, layout)[1]
     cap = _heads("k_cache", k_cache, layout)[2]
-    _view("q", q, q.shape, dt, dev)
+    _rows_consecutive("q", q)
     _view("k", k, _shape(B, Hkv, S, D, layout), dt, dev)
     _view("v", v, k.shape, dt, dev)
     _view("k_cache", k_cache, _shape(B, Hkv, cap, D, layout), dt, dev)
@@ -305,30 +308,23 @@ def rope_append(q, k, v, k_cache, v_cache, lens, freqs, counts=None, window: int
         raise TypeError("freqs must be a 1-d float64 tensor (rope_frequencies)")
     _plain("freqs", freqs, freqs.shape, _F64, dev)
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        q_out = q.new_empty(q.shape)
     else:
         _view("q_out", q_out, q.shape, dt, dev)
     if k_out is None:
-        k_out = torch.empty(k.shape, dtype=dt, device=dev)
+        k_out = k.new_empty(k.shape)
     else:
         _view("k_out", k_out, k.shape, dt, dev)
     strides = _strides((q, k, v, q_out, k_out, k_cache, v_cache), layout)
-    with _current(dev):
-        st = lib().cattn_rope_append(_ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_out), _ptr(k_cache),
-                                     _ptr(v_cache), _ptr(lens), _ptr(counts), _ptr(freqs), B, S, Hq, Hkv, D,
-                                     2 * freqs.shape[0], cap, int(window), int(sinks), int(bool(rolling)), strides,
-                                     _LAYOUTS[layout], int(bool(interleaved)), float(amplitude), code, _stream(dev))
-    _done(st, "cattn_rope_append")
+    _run("cattn_rope_append", dev, _at(q), _at(k), _at(v), _at(q_out), _at(k_out), _at(k_cache), _at(v_cache),
+         _at(lens), _at(counts), _at(freqs), _int(B), _int(S), Hq, Hkv, D, 2 * freqs.shape[0], _int(cap), _int(window),
+         _int(sinks), bool(rolling), strides, _LAYOUTS[layout], bool(interleaved), amplitude, code)
     return q_out, k_out
 
 
 # ---------------------------------------------------------------------------
 # Sliding-window attention with sinks
 # ---------------------------------------------------------------------------
-def _int32(n: int) -> int:
-    return min(int(n), 2 ** 31 - 1)
-
-
 def swa_fwd(q, k, v, scale: float, window: int, sinks: int = 0, lens=None, layout: str = "bhsd", o=None, lse=None):
     """O, LSE of causal attention in which query i sees key j iff i - j < window or j < sinks.
 
@@ -341,28 +337,25 @@ def swa_fwd(q, k, v, scale: float, window: int, sinks: int = 0, lens=None, layou
     code = _dtype_code(q)
     dev, dt = q.device, q.dtype
     Hkv = _heads("k", k, layout)[1]
-    _view("q", q, q.shape, dt, dev)
+    _rows_consecutive("q", q)
     _view("k", k, _shape(B, Hkv, S, D, layout), dt, dev)
     _view("v", v, k.shape, dt, dev)
     _batch("lens", lens, B, dev)
     if o is None:
-        o = torch.empty(q.shape, dtype=dt, device=dev)
+        o = q.new_empty(q.shape)
     else:
         _view("o", o, q.shape, dt, dev)
     if lse is None:
         lse = torch.empty((B, Hq, S), dtype=_F32, device=dev)
     else:
         _plain("lse", lse, (B, Hq, S), _F32, dev)
-    with _current(dev):
-        st = lib().cattn_swa_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(lens), B, Hq, Hkv, S, D,
-                                 _int32(window), _int32(sinks), float(scale), _strides((q, k, v, o), layout),
-                                 _LAYOUTS[layout], code, _stream(dev))
-    _done(st, "cattn_swa_fwd")
+    _run("cattn_swa_fwd", dev, _at(q), _at(k), _at(v), _at(o), _at(lse), _at(lens), B, Hq, Hkv, _int(S), D,
+         _int(window), _int(sinks), scale, _strides((q, k, v, o), layout), _LAYOUTS[layout], code)
     return o, lse
 
 
 def swa_bwd_workspace_bytes(B: int, Hq: int, Hkv: int, S: int, D: int, window: int, sinks: int = 0) -> int:
-    return int(lib().cattn_swa_bwd_workspace_bytes(B, Hq, Hkv, S, D, _int32(window), _int32(sinks)))
+    return int(lib().cattn_swa_bwd_workspace_bytes(B, Hq, Hkv, S, D, _int(window), _int(sinks)))
 
 
 def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens=None, layout: str = "bhsd",
@@ -373,33 +366,30 @@ def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens
     dev, dt = q.device, q.dtype
     Hkv = _heads("k", k, layout)[1]
     kv = _shape(B, Hkv, S, D, layout)
-    for n, t, shape in (("q", q, q.shape), ("k", k, kv), ("v", v, kv), ("o", o, q.shape), ("do", do, q.shape)):
+    _rows_consecutive("q", q)
+    for n, t, shape in (("k", k, kv), ("v", v, kv), ("o", o, q.shape), ("do", do, q.shape)):
         _view(n, t, shape, dt, dev)
     _plain("lse", lse, (B, Hq, S), _F32, dev)
     _batch("lens", lens, B, dev)
     for n, t, shape in (("dq", dq, q.shape), ("dk", dk, kv), ("dv", dv, kv)):
         if t is not None:
             _view(n, t, shape, dt, dev)
-    # (no rows: the sums are over nothing)
-    dq = torch.empty(q.shape, dtype=dt, device=dev) if dq is None else dq
-    dk = torch.empty(kv, dtype=dt, device=dev) if dk is None else dk
-    dv = torch.empty(kv, dtype=dt, device=dev) if dv is None else dv
+    dq = q.new_empty(q.shape) if dq is None else dq
+    dk = q.new_empty(kv) if dk is None else dk
+    dv = q.new_empty(kv) if dv is None else dv
     n = swa_bwd_workspace_bytes(B, Hq, Hkv, S, D, window, sinks) // 4
     if workspace is None:
-        workspace = torch.empty((n,), dtype=_F32, device=dev)
+        workspace = lse.new_empty(n)
     else:
         _check_workspace(workspace, n, dev)
-    with _current(dev):
-        st = lib().cattn_swa_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(do), _ptr(lse), _ptr(lens), _ptr(dq),
-                                 _ptr(dk), _ptr(dv), _ptr(workspace), B, Hq, Hkv, S, D, _int32(window),
-                                 _int32(sinks), float(scale), _strides((q, k, v, o, do, dq, dk, dv), layout),
-                                 _LAYOUTS[layout], code, _stream(dev))
-    _done(st, "cattn_swa_bwd")
+    _run("cattn_swa_bwd", dev, _at(q), _at(k), _at(v), _at(o), _at(do), _at(lse), _at(lens), _at(dq), _at(dk), _at(dv),
+         _at(workspace), B, Hq, Hkv, _int(S), D, _int(window), _int(sinks), scale,
+         _strides((q, k, v, o, do, dq, dk, dv), layout), _LAYOUTS[layout], code)
     return dq, dk, dv
 
 
 def swa_decode_workspace_bytes(B: int, Hq: int, Hkv: int, cap: int, D: int, window: int, sinks: int = 0) -> int:
-    return int(lib().cattn_swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, _int32(window), _int32(sinks)))
+    return int(lib().cattn_swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, _int(window), _int(sinks)))
 
 
 def swa_decode(q, k_cache, v_cache, lens, scale: float, window: int, sinks: int = 0, rolling: bool = False,
@@ -418,12 +408,12 @@ def swa_decode(q, k_cache, v_cache, lens, scale: float, window: int, sinks: int 
     code = _dtype_code(q)
     dev, dt = q.device, q.dtype
     _, Hkv, cap, _ = _heads("k_cache", k_cache, layout)
-    _view("q", q, q.shape, dt, dev)
+    _rows_consecutive("q", q)
     _view("k_cache", k_cache, _shape(B, Hkv, cap, D, layout), dt, dev)
     _view("v_cache", v_cache, k_cache.shape, dt, dev)
     _plain("lens", lens, (B,), _I32, dev)
     if o is None:
-        o = torch.empty((B, Hq, D), dtype=dt, device=dev)
+        o = q.new_empty(q.shape)
     else:
         _view("o", o, q.shape, dt, dev)
     if lse is None:
@@ -432,13 +422,10 @@ def swa_decode(q, k_cache, v_cache, lens, scale: float, window: int, sinks: int 
         _plain("lse", lse, (B, Hq), _F32, dev)
     n = swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, window, sinks) // 4
     if workspace is None:
-        workspace = torch.empty((n,), dtype=_F32, device=dev) if n else None
+        workspace = lse.new_empty(n) if n else None
     else:
         _check_workspace(workspace, n, dev)
-    with _current(dev):
-        st = lib().cattn_swa_decode(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(o), _ptr(lse), _ptr(lens),
-                                    _ptr(workspace), B, Hq, Hkv, cap, D, _int32(window), _int32(sinks),
-                                    int(bool(rolling)), float(scale), _strides((q, k_cache, v_cache, o), layout),
-                                    _LAYOUTS[layout], code, _stream(dev))
-    _done(st, "cattn_swa_decode")
+    _run("cattn_swa_decode", dev, _at(q), _at(k_cache), _at(v_cache), _at(o), _at(lse), _at(lens), _at(workspace), B,
+         Hq, Hkv, _int(cap), D, _int(window), _int(sinks), bool(rolling), scale,
+         _strides((q, k_cache, v_cache, o), layout), _LAYOUTS[layout], code)
     return o, lse

@@ -247,7 +247,7 @@ static cattn_status rope_sizes(int B, int S, int Hq, int Hkv, int D, int rot, in
   if (D <= 0 || rot <= 0 || rot % 2 || rot > D) return fail(CATTN_ERR_INVALID_ARG, "rot must be even, 2 .. D");
   if (!isfinite(amplitude)) return fail(CATTN_ERR_INVALID_ARG, "amplitude must be finite");
   if (D % 2 || D > 512) return fail(CATTN_ERR_UNSUPPORTED, "D must be even and at most 512");
-  if ((int64_t)B * S > INT_MAX || (int64_t)8 * (Hq + (int64_t)Hkv) > (1 << 20))
+  if ((int64_t)B * S >= INT_MAX || (int64_t)8 * (Hq + (int64_t)Hkv) > (1 << 20))
     return fail(CATTN_ERR_UNSUPPORTED, "problem too large");
   return CATTN_OK;
 }
