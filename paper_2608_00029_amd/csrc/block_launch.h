@@ -97,27 +97,36 @@ struct SwaDecodeArgs {
 
 constexpr int64_t kSwaCus = 256;  // compute units of the one GPU these kernels are built for
 
-// dK and dV of the sink keys.  Their queries outside the window (`far`: there
-// are some where S > window) reach to the end of the sequence, however long,
-// while every other key has window queries: the far (query head, 32-query tile)
-// pairs of a 32-key tile of sinks are cut into this many parts, so that the
+// dK and dV of the sink keys.  Their queries outside the window reach to the end
+// of the sequence, however long, while every other key has window queries.
+// Where those far queries of all heads of a group are many, the window's work
+// groups leave them out, and a grid of their own takes them: the far (query head,
+// 32-query tile) pairs of a 32-key tile of sinks cut into parts, so that the
 // parts of all heads give the GPU one work group per CU (what its LDS holds at D
-// = 128), but a part has at least eight tiles.  Each part leaves float32 partial
-// sums.
-constexpr bool swa_has_far(int S, int window, int sinks) { return sinks > 0 && S > window; }
+// = 128), but a part has at least a tile for each of its waves.  Each part leaves
+// float32 partial sums.  Backward, 4 sinks, us, with a grid of their own /
+// without, by far queries times heads of the group:
+//   bf16  256: B1 H4 S1024 D64 35.6 / 27.0;  384: B4 H8 S512 D128 39.6 / 34.5;
+//         768: B1 H4 S1024 D64 28.1 / 25.6, B4 H8 S1024 D128 60.4 / 74.8;
+//         1536: B1 H16/4 S512 D64 30.6 / 37.3;  14336: B1 H16/4 S4096 D128 119 / 475
+//   f32   277: B1 H4 S777 D64 65.2 / 62.1;  381: B1 H12/4 S777 D64 131 / 128;
+//         577: B1 H4 S777 D64 45.4 / 57.5;  831: B1 H12/4 S777 D64 108 / 126
+constexpr bool swa_has_far(bool bf16, int Hq, int Hkv, int S, int window, int sinks) {
+  return sinks > 0 && (int64_t)(Hq / Hkv) * (S - window) > (bf16 ? 512 : 400);
+}
 constexpr int swa_sink_tiles(int S, int sinks) { return ((sinks < S ? sinks : S) + 31) / 32; }
-constexpr int swa_far_parts(int B, int Hq, int Hkv, int S, int window, int sinks) {
-  if (!swa_has_far(S, window, sinks)) return 0;
+constexpr int swa_far_parts(bool bf16, int B, int Hq, int Hkv, int S, int window, int sinks) {
+  if (!swa_has_far(bf16, Hq, Hkv, S, window, sinks)) return 0;
   const int64_t tiles = (int64_t)(Hq / Hkv) * ((S - window + 31) / 32 + 1);
-  const int64_t want = kSwaCus / ((int64_t)B * Hkv * swa_sink_tiles(S, sinks)), most = (tiles + 7) / 8;
+  const int64_t want = kSwaCus / ((int64_t)B * Hkv * swa_sink_tiles(S, sinks)), most = (tiles + 3) / 4;
   const int64_t n = want < most ? want : most;
   return n < 1 ? 1 : (int)n;
 }
 // Floats of the far area: [B * Hkv][sink tile][1 + parts][dK, dV][32][D]; slot 0
-// is the window's own sum.
+// is the window's own sum.  (Of either type: what float32 needs.)
 constexpr int64_t swa_far_floats(int B, int Hq, int Hkv, int S, int D, int window, int sinks) {
-  if (!swa_has_far(S, window, sinks)) return 0;
-  return (int64_t)B * Hkv * swa_sink_tiles(S, sinks) * (1 + swa_far_parts(B, Hq, Hkv, S, window, sinks)) * 2 * 32 * D;
+  const int parts = swa_far_parts(false, B, Hq, Hkv, S, window, sinks);
+  return parts ? (int64_t)B * Hkv * swa_sink_tiles(S, sinks) * (1 + parts) * 2 * 32 * D : 0;
 }
 
 // Decoding: parts that the visible slots of one (sequence, key/value head) are

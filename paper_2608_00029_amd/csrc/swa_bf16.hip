@@ -22,6 +22,8 @@
 //  * Padded batches: rows from lens[b] on are never read (a tile that reaches
 //    past the end repeats the last row, masked), so they may hold anything;
 //    their O and gradients are 0 and their LSE -inf.
+#include <limits.h>
+
 #include <algorithm>
 #include <utility>
 
@@ -223,7 +225,7 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
       if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (!swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks)) s[e] = -INFINITY;
+          s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
       }
       f32x16 pv;
       float psum = block_exp(s, c, m * c, pv);
@@ -447,7 +449,7 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
       if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (!swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks)) s[e] = -INFINITY;
+          s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) dx[e] = -exp2_hw(fmaf(s[e], c, -lse2)) * dx[e];  // dS^T = P (dP - D)
@@ -494,11 +496,12 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   const int b = bkv / a.Hkv, hk = bkv - b * a.Hkv;
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int k0 = kt * BKV, kw = k0 + 32 * kg, my_k = kw + r;
-  const bool far = FAR || swa_has_far(a.S, a.window, a.sinks);  // sink keys' sums go to the far area
+  const bool far = FAR || swa_has_far(true, a.Hq, a.Hkv, a.S, a.window, a.sinks);  // sink keys' sums go to the far area
+  const int sinks = far ? 0 : a.sinks;  // the sinks whose far queries this kernel walks itself
 
   // query tiles jlo .. jhi of every head of the group see a key of this work group
   const int jlo = FAR ? (k0 + a.window) / 32 : k0 / 32;
-  const int jhi = FAR ? (len - 1) / 32 : (min(len, min(k0 + BKV, len) + a.window - 1) - 1) / 32;
+  const int jhi = FAR || k0 < sinks ? (len - 1) / 32 : (min(len, min(k0 + BKV, len) + a.window - 1) - 1) / 32;
   const int nj = (FAR ? k0 + a.window < len : k0 < len) ? jhi - jlo + 1 : 0;
   int n = group * nj, x0 = 0;
   if constexpr (FAR) {
@@ -569,7 +572,9 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
       if (i * SPLIT + part >= n) return;
       const int qs = jc * 32;
       advance(jc, SPLIT);
-      if (FAR ? qs + 31 - kw < a.window : kw >= len || qs + 31 < kw || qs - (kw + 31) >= a.window) return;
+      if (FAR ? qs + 31 - kw < a.window
+              : kw >= len || qs + 31 < kw || (qs - (kw + 31) >= a.window && kw >= sinks))
+        return;
       const char* lq = ring + sl * SETB;
       const char* ldo = lq + TILE;
       const float* llse = (const float*)(aux + sl * AUX);
@@ -600,11 +605,14 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
       // s[e], dx[e]: S - LSE/scale and D - dP of query qs + acc_row(e, h), key my_k
       const bool masked = FAR ? qs - (kw + 31) < a.window || kw + 32 > a.sinks : qs < kw + 31 || qs + 31 - kw >= a.window;
       if (masked || qs + 32 > len) {
+        int key = my_k;
+        asm volatile("" : "+v"(key));  // (what follows is not hoisted out of the rare branch into registers)
+        const int low = FAR ? a.window : 0;  // the pair counts where low <= query - key < high
+        const int high = FAR ? (key < a.sinks ? INT_MAX : 0) : key < sinks ? INT_MAX : a.window;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int ahead = qs + acc_row(e, h) - my_k;
-          const bool in = FAR ? ahead >= a.window && my_k < a.sinks : ahead >= 0 && ahead < a.window;
-          if (!in || qs + acc_row(e, h) >= len) s[e] = -INFINITY;
+          const int qry = qs + acc_row(e, h), ahead = qry - key;
+          s[e] = swa_masked((ahead >= low) & (ahead < high) & (qry < len), s[e]);
         }
       }
 #pragma unroll
@@ -744,7 +752,7 @@ template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
 }
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
-  const int far = swa_far_parts(a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const int far = swa_far_parts(true, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
   hipError_t e;
   switch (form_of(Pass::kDq, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
     case kFour: e = dq_s<D, 4, 4, 2>(a, c, st); break;
@@ -772,7 +780,7 @@ template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_swa_far_sum(const SwaArgs& a, hipStream_t st) {
-  const int far = swa_far_parts(a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const int far = swa_far_parts(a.bf16, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
   const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * (a.sinks < a.S ? a.sinks : a.S)), 2);
   if (a.bf16) hipLaunchKernelGGL((swa_far_sum_kernel<bf16>), grid, dim3(256), 0, st, a, far);
   else hipLaunchKernelGGL((swa_far_sum_kernel<float>), grid, dim3(256), 0, st, a, far);

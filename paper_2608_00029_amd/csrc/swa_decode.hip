@@ -210,7 +210,7 @@ __global__ __launch_bounds__(256) void swa_decode_bf16_kernel(SwaDecodeArgs a, f
       if (count < 32) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (acc_row(e, h) >= count) s[e] = -INFINITY;
+          s[e] = swa_masked(acc_row(e, h) < count, s[e]);
       }
       online_softmax(s, c, run, [&](float alpha) {
 #pragma unroll
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void swa_decode_f32_kernel(SwaDecodeArgs a, fl
     if (count < 32) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (acc_row(e, h) >= count) s[e] = -INFINITY;
+        s[e] = swa_masked(acc_row(e, h) < count, s[e]);
     }
     online_softmax(s, c, run, [&](float alpha) {
 #pragma unroll
@@ -315,6 +315,9 @@ __global__ __launch_bounds__(256) void swa_decode_join_kernel(SwaDecodeArgs a, i
   const f32x4* p = (const f32x4*)a.ws + (int64_t)bh * quads + q;
   f32x2 st{0.f, 0.f};
   if (tid < parts) st = *(const f32x2*)(a.ws + parts * heads * a.D + 2 * (tid * heads + bh));
+  f32x4 ahead[4];  // the first rows, on their way while the weights are formed
+#pragma unroll
+  for (int u = 0; u < 4; ++u) ahead[u] = s0 + u * n < parts ? p[(s0 + u * n) * heads * quads] : f32x4{};
   const float m = wave_max(st[1] == 0.f ? -INFINITY : st[0]);  // (sum 0: the part saw no slot)
   if ((tid & 63) == 0) red[0][w] = m;
   __syncthreads();
@@ -326,11 +329,11 @@ __global__ __launch_bounds__(256) void swa_decode_join_kernel(SwaDecodeArgs a, i
   __syncthreads();
   const float l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
   f32x4 v{};
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (s0 + u * n < parts) v += ahead[u] * weight[s0 + u * n];
 #pragma unroll 4
-  for (int s = s0; s < parts; s += n) {
-    const float g = weight[s];
-    if (g != 0.f) v += p[(int64_t)s * heads * quads] * g;  // (a part without slots holds 0 at weight 0: not read)
-  }
+  for (int s = s0 + 4 * n; s < parts; s += n) v += p[s * heads * quads] * weight[s];
   sums[tid] = v;
   __syncthreads();
   if (s0) return;

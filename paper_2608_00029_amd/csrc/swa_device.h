@@ -19,9 +19,13 @@ __device__ __forceinline__ int swa_len(const int* lens, int b, int S) { return l
 // tiles in one L2.
 __device__ __forceinline__ int swa_head(int i, int n) { return n % 8 == 0 ? (i & 7) * (n >> 3) + (i >> 3) : i; }
 
+// Masks are selects of conditions joined by & and |.  With && and || the compiler
+// (ROCm 7.2's) made branches of them, and in one kernel lost the assignment of an
+// accumulator's first element in the branch: hidden pairs kept their score.
 __device__ __forceinline__ bool swa_sees(int query, int key, int window, int sinks) {
-  return key <= query && (query - key < window || key < sinks);
+  return (key <= query) & ((query - key < window) | (key < sinks));
 }
+__device__ __forceinline__ float swa_masked(bool seen, float score) { return seen ? score : -INFINITY; }
 
 // The 32-key tiles that queries [q0, q1) see: the sinks' tiles 0 .. sink_tiles-1,
 // then first .. first + n - sink_tiles - 1.

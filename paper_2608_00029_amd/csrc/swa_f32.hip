@@ -6,6 +6,8 @@
 // the fixed operand in LDS.  Which tiles are visited and masked, grouped heads,
 // the sinks' far queries and padded batches are as in the bf16 kernels
 // (swa_bf16.hip).
+#include <limits.h>
+
 #include "attn_launch.h"
 #include "f32_stream.h"
 #include "swa_device.h"
@@ -68,7 +70,7 @@ void swa_fwd_f32_kernel(SwaArgs a, float c) {
     if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (!swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks)) s[e] = -INFINITY;
+        s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
     }
     float mx = s[0];
 #pragma unroll
@@ -203,7 +205,7 @@ void swa_dq_f32_kernel(SwaArgs a, float c) {
     if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (!swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks)) s[e] = -INFINITY;
+        s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = exp2_hw(fmaf(s[e], c, -lse2)) * (dp[e] - Dq);  // dS^T
@@ -229,10 +231,11 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
   const int b = bkv / a.Hkv, hk = bkv - b * a.Hkv;
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int kw = kt * 32, my_k = kw + r;
-  const bool far = FAR || swa_has_far(a.S, a.window, a.sinks);
+  const bool far = FAR || swa_has_far(false, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const int sinks = far ? 0 : a.sinks;  // the sinks whose far queries this kernel walks itself
 
   const int jlo = FAR ? (kw + a.window) / 32 : kt;
-  const int jhi = FAR ? (len - 1) / 32 : (min(len, min(kw + 32, len) + a.window - 1) - 1) / 32;
+  const int jhi = FAR || kw < sinks ? (len - 1) / 32 : (min(len, min(kw + 32, len) + a.window - 1) - 1) / 32;
   const int nj = (FAR ? kw + a.window < len : kw < len) ? jhi - jlo + 1 : 0;
   int n = group * nj, x0 = 0;
   if constexpr (FAR) {
@@ -298,11 +301,12 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
     f32x16 dp = contract_rows<D, 16>(dor, vf, lane, f32x16{}, [&](int e) { dot[e] = dOm.trans_step(q0, e); });
     const bool masked = FAR ? q0 - (kw + 31) < a.window || kw + 32 > a.sinks : q0 < kw + 31 || q0 + 31 - kw >= a.window;
     if (masked || q0 + 32 > len) {
+      const int low = FAR ? a.window : 0;  // the pair counts where low <= query - key < high
+      const int high = FAR ? (my_k < a.sinks ? INT_MAX : 0) : my_k < sinks ? INT_MAX : a.window;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int qry = q0 + acc_row(e, h), ahead = qry - my_k;
-        const bool in = FAR ? ahead >= a.window && my_k < a.sinks : ahead >= 0 && ahead < a.window;
-        if (!in || qry >= len) s[e] = -INFINITY;
+        s[e] = swa_masked((ahead >= low) & (ahead < high) & (qry < len), s[e]);
       }
     }
 #pragma unroll
@@ -346,7 +350,7 @@ template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
   const int64_t tiles = (a.S + 31) / 32;
-  const int far = swa_far_parts(a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const int far = swa_far_parts(false, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
   hipLaunchKernelGGL((swa_dq_f32_kernel<D>), dim3((unsigned)(a.B * a.Hq * tiles)), dim3(256), 0, st, a, c);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -145,9 +145,12 @@ def test_workspace_sizes(lib):
     rows = 2 * 2 * 4 * 64 * 4
     assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 40, 64, 40, 2) == rows  # the window covers the sequence
     assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 40, 64, 8, 0) == rows   # no sinks
-    far = cattn.swa_bwd_workspace_bytes(2, 4, 2, 40, 64, 8, 2) - rows
+    assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 40, 64, 8, 2) == rows   # few queries that only the sinks see
+    rows = 2 * 2 * 4 * 608 * 4
+    assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 600, 64, 400, 2) == rows
+    far = cattn.swa_bwd_workspace_bytes(2, 4, 2, 600, 64, 8, 2) - rows
     assert far > 0 and far % (2 * 2 * 2 * 32 * 64 * 4) == 0
-    assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 40, 64, 8, 2 ** 40) > rows  # clamped to the sequence
+    assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 600, 64, 8, 2 ** 40) > rows  # clamped to the sequence
     assert cattn.swa_bwd_workspace_bytes(2, 3, 2, 40, 64, 8, 2) == 0
     assert cattn.swa_decode_workspace_bytes(300, 8, 8, 4096, 64, 4000) == 0  # work groups enough without parts
     one = cattn.swa_decode_workspace_bytes(1, 8, 2, 4096, 64, 4000)

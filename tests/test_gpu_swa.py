@@ -94,6 +94,17 @@ def test_grids_of_every_split(cuda, D, B, Hq, Hkv, S, window, sinks):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,S,window,sinks", [
+    (2, 2, 520, 8, 1), (2, 2, 521, 8, 1),      # 512 far queries and one more: without and with a grid of their own
+    (2, 1, 300, 100, 2), (2, 1, 302, 101, 2),  # the same at 400, where float32 changes
+    (4, 1, 700, 33, 40), (3, 3, 900, 128, 70), (8, 1, 350, 1, 32)])
+def test_far_queries_of_the_sinks(cuda, Hq, Hkv, S, window, sinks, D, dtype):
+    check(cuda, 1, Hq, Hkv, S, D, window, sinks, dtype)
+    check(cuda, 3, Hq, Hkv, S, D, window, sinks, dtype, lens=[S, window, S // 2 + 3])  # far queries in some sequences only
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ends_of_the_softmax(cuda, dtype):
     """Uniform rows, and rows near one-hot whose offset moves."""
     check(cuda, 1, 2, 2, 140, 64, 50, 2, dtype, scale=1e-20)
