@@ -12,6 +12,7 @@ allocated here are contiguous.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional
 
 import torch
@@ -178,6 +179,7 @@ def rmsnorm_fwd_q8(x, gamma, residual=None, eps: float = 1e-5, group: int = 0):
     return q, scale, x if h is None else h, rstd
 
 
+@functools.lru_cache(maxsize=256)  # (a call into the library each time costs 1 us)
 def rmsnorm_bwd_workspace_bytes(rows: int, C: int) -> int:
     return int(lib().cattn_rmsnorm_bwd_workspace_bytes(rows, C))
 
@@ -354,6 +356,7 @@ def swa_fwd(q, k, v, scale: float, window: int, sinks: int = 0, lens=None, layou
     return o, lse
 
 
+@functools.lru_cache(maxsize=256)
 def swa_bwd_workspace_bytes(B: int, Hq: int, Hkv: int, S: int, D: int, window: int, sinks: int = 0) -> int:
     return int(lib().cattn_swa_bwd_workspace_bytes(B, Hq, Hkv, S, D, _int(window), _int(sinks)))
 
@@ -388,6 +391,7 @@ def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens
     return dq, dk, dv
 
 
+@functools.lru_cache(maxsize=256)
 def swa_decode_workspace_bytes(B: int, Hq: int, Hkv: int, cap: int, D: int, window: int, sinks: int = 0) -> int:
     return int(lib().cattn_swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, _int(window), _int(sinks)))
 

@@ -37,14 +37,20 @@ template <typename T, int V> __device__ __forceinline__ typename Floats<V>::type
   }
   return f;
 }
-template <typename T, int V> __device__ __forceinline__ void store_v(T* p, typename Floats<V>::type f) {
-  if constexpr (sizeof(T) == 2 && V == 8) {
-    bf16x8 v;
+template <typename T, int V, bool NT = false>
+__device__ __forceinline__ void store_v(T* p, typename Floats<V>::type f) {
+  if constexpr (V * sizeof(T) == 16) {
+    u32x4 u;
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (__bf16)f[e];
-    *(bf16x8*)p = v;
-  } else if constexpr (sizeof(T) == 4 && V == 4) {
-    *(f32x4*)p = f;
+      for (int e = 0; e < 8; ++e) v[e] = (__bf16)f[e];
+      u = __builtin_bit_cast(u32x4, v);
+    } else {
+      u = __builtin_bit_cast(u32x4, f);
+    }
+    if constexpr (NT) __builtin_nontemporal_store(u, (u32x4*)p);
+    else *(u32x4*)p = u;
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) p[e] = (T)f[e];
@@ -189,8 +195,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int tpg, int item
     if (APPEND && !k.active) y = z = Vec{};
     const bool two = !INTER && turned;
     if (turned || !(is_q ? a.in_place_q : a.in_place_k) || !k.active) {  // (else it is where it belongs)
-      store_v<T, V>(dst + col, y);
-      if (two) store_v<T, V>(dst + col + half, z);
+      store_v<T, V, !APPEND>(dst + col, y);
+      if (two) store_v<T, V, !APPEND>(dst + col + half, z);
     }
     if (APPEND && cache) {
       store_v<T, V>(cache + col, y);

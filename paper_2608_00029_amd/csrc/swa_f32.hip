@@ -39,13 +39,21 @@ void swa_fwd_f32_kernel(SwaArgs a, float c) {
   const int bh = swa_head(blockIdx.x % BH, BH), qt = n_qtiles - 1 - blockIdx.x / BH;
   const int b = bh / a.Hq, hq = bh - b * a.Hq, hk = hq / (a.Hq / a.Hkv);
   const int len = swa_len(a.lens, b, a.S), qw = qt * 32, my_q = qw + r;
-  float* orow = (float*)a.out + b * a.so.b + hq * a.so.h + my_q * a.so.s;
-  float* lse = a.lse + (int64_t)bh * a.S + my_q;
+  // (pointers from an opaque copy of the row, formed where they are used)
+  auto out_row = [&](int q) {
+    asm volatile("" : "+v"(q));
+    return (float*)a.out + b * a.so.b + hq * a.so.h + q * a.so.s;
+  };
+  auto put_lse = [&](int q, float v) {
+    asm volatile("" : "+v"(q));
+    a.lse[(int64_t)bh * a.S + q] = v;
+  };
   if (w == 0 && my_q >= len && my_q < a.S) {  // a row without keys
     const ColBlocks<D> zero{};
+    float* orow = out_row(my_q);
 #pragma unroll
     for (int g = 0; g < 4; ++g) store_cols<D>(orow, g, h, zero, 0.f);
-    if (h == 0) *lse = -INFINITY;
+    if (h == 0) put_lse(my_q, -INFINITY);
   }
   if (qw >= len) return;
   const KeyTiles kt(qw, min(len, qw + 32), a.window, a.sinks);
@@ -121,8 +129,8 @@ void swa_fwd_f32_kernel(SwaArgs a, float c) {
 #pragma unroll
     for (int p = 1; p < 4; ++p) v.b[dt] += get_partial<D>(sm, p, dt, w, lane) * sp[p];
   }
-  store_cols<D>(orow, w, h, v, 1.0f / l);
-  if (w == 0 && h == 0) *lse = (mn * c + log2f(l)) * kLn2;
+  store_cols<D>(out_row(my_q), w, h, v, 1.0f / l);
+  if (w == 0 && h == 0) put_lse(my_q, (mn * c + log2f(l)) * kLn2);
 }
 
 // The four parts' accumulators, added in order through `area`: f(index group of
