@@ -292,31 +292,38 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void rmsnorm_bwd_kernel(RmsBw
   }
 }
 
-// dgamma: work group k sums the 8 column quads 8k .. 8k+7 over the partial rows.
-// Lane l of wave w takes quad 8k + (l & 7) of rows 8w + (l >> 3) + 128 i; the
-// eight row streams of a wave meet in a fixed butterfly, then wave 0 adds the
+// dgamma: work group k sums the 4 column quads 4k .. 4k+3 over the partial rows.
+// Lane l of wave w takes quad 4k + (l & 3) of rows 16w + (l >> 2) + 256 i; the
+// sixteen row streams of a wave meet in a fixed butterfly, then wave 0 adds the
 // 16 waves' sums in order.
 __global__ __launch_bounds__(1024) void rmsnorm_bwd_sum_kernel(const float* __restrict__ part,
                                                                float* __restrict__ dgamma, int n_part, int C) {
-  __shared__ f32x4 red[16][8];
+  __shared__ f32x4 red[16][4];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int C4 = C >> 2, q = blockIdx.x * 8 + (lane & 7);
+  const int C4 = C >> 2, q = blockIdx.x * 4 + (lane & 3);
   const bool ok = q < C4;
+  const f32x4* p = (const f32x4*)part + q;
   f32x4 s = f32x4{};
-  if (ok)
-    for (int i = 8 * w + (lane >> 3); i < n_part; i += 128) s += ((const f32x4*)part)[(int64_t)i * C4 + q];
+  if (ok) {
+    const int i = 16 * w + (lane >> 2);
+    // at most 512 partial rows: two per stream
+    const f32x4 a = i < n_part ? p[(int64_t)i * C4] : f32x4{}, b = i + 256 < n_part ? p[(int64_t)(i + 256) * C4] : f32x4{};
+    s = a + b;
+  }
 #pragma unroll
-  for (int d = 8; d < 64; d <<= 1)
+  for (int d = 4; d < 64; d <<= 1)
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[e] += __shfl_xor(s[e], d, 64);
-  if (lane < 8) red[w][lane] = s;
+  if (lane < 4) red[w][lane] = s;
   __syncthreads();
-  if (w == 0 && lane < 8 && ok) {
+  if (w == 0 && lane < 4 && ok) {
     f32x4 t = red[0][lane];
+#pragma unroll
     for (int i = 1; i < 16; ++i) t += red[i][lane];
     ((f32x4*)dgamma)[q] = t;
   }
 }
+static_assert(rms_bwd_groups(1 << 30) == 512, "two partial rows per stream");
 
 // Waves per row and steps per lane: as many waves as keep a row at four steps
 // or fewer, and more where there are too few rows to fill the GPU with them
@@ -380,7 +387,7 @@ template <typename T> hipError_t bwd_t(const RmsBwd& a, hipStream_t st) {
   const int oct = a.C / 8;
   hipError_t e = oct <= 2 * 64 ? bwd_w<T, 1>(a, st) : oct <= 8 * 64 ? bwd_w<T, 4>(a, st) : bwd_w<T, 16>(a, st);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(rmsnorm_bwd_sum_kernel, dim3((unsigned)((a.C / 4 + 7) / 8)), dim3(1024), 0, st,
+  hipLaunchKernelGGL(rmsnorm_bwd_sum_kernel, dim3((unsigned)((a.C / 4 + 3) / 4)), dim3(1024), 0, st,
                      (const float*)a.part, a.dgamma, rms_bwd_groups(a.rows), a.C);
   return hipGetLastError();
 }
