@@ -37,40 +37,123 @@ namespace {
 
 constexpr float kSumMax = 4294967296.0f;  // bound of a block's probability sum before the offset moves
 
+// dma16 to LDS byte address lds + OFF: the sum is formed in M0, so that the many
+// targets of an unrolled ring take one scalar register and not one each.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+template <int OFF> __device__ __forceinline__ void dma16_at(const void* sbase, unsigned voff, unsigned lds) {
+  asm volatile("s_add_u32 m0, %0, %3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(sbase), "i"(OFF)
+               : "memory", "m0", "scc");
+}
+#pragma clang diagnostic pop
+
 // HBM -> LDS copies of pairs of 32-row tiles (K and V, or Q and dO) by a work
-// group of W waves; rows past `last` repeat row `last`.  A wave copies 1 KB
-// pieces: with more waves than a tile has pieces, the first half of them takes
-// one tile and the others the other.  The offsets of a lane's chunks are formed
-// at each copy (a minimum and a multiply-add each), for any row stride below 2^23.
-template <int D, int W> struct SwaCopy {
-  static constexpr int PIECES = TileGeom<D>::TILE / 1024, CPR = TileGeom<D>::CPR;
+// group of W waves.  A wave copies 1 KB pieces: with more waves than a tile has
+// pieces, the first half of them takes one tile and the others the other.  A
+// lane's offsets inside a tile are fixed for the kernel; a tile that reaches past
+// the sequence's end, whose rows past row `last` repeat it, forms its own.
+// (Row strides stay below 2^23: 24-bit products.)  TIGHT, for dK/dV at D = 128,
+// whose registers are all in use: one register per tensor and one for the chunk
+// instead of two per tensor, an addition of three terms per copy.
+template <int D, int W, bool TIGHT = false> struct SwaCopy {
+  static constexpr int TILE = TileGeom<D>::TILE, PIECES = TILE / 1024, CPR = TileGeom<D>::CPR;
   static constexpr bool BOTH = W <= PIECES;  // every wave copies from both tiles
   static constexpr int N = BOTH ? PIECES / W : 1, STEP = 64 * W / CPR;
   static constexpr int PER_PAIR = BOTH ? 2 * N : 1;  // copies of each wave
   static_assert(BOTH || W == 2 * PIECES, "one piece per wave");
-  unsigned row, chunk[N], at;
-  bool second;
-  __device__ __forceinline__ void init(int w, int lane) {
-    second = !BOTH && w >= PIECES;
-    const int p = (BOTH ? w : w % PIECES) * 64 + lane;
-    row = p / CPR;
-    at = (BOTH ? w : w % PIECES) * 1024;
-#pragma unroll
-    for (int i = 0; i < N; ++i) chunk[i] = ((p % CPR) ^ swz(row + STEP * i)) << 4;
+  static_assert(!TIGHT || (N == 2 && STEP == 16), "the second copy's rows are 16 on: swz(row + 16) = swz(row) ^ 7");
+  unsigned va[TIGHT ? 1 : N], vb[TIGHT ? 1 : N];  // byte offsets of this lane's chunks (vb: BOTH only); TIGHT: its row's
+  unsigned chunk;                                 // TIGHT: the chunk's offset in the row
+  unsigned lds;  // where this wave's first piece goes
+  int w, rsa, rsb;
+  __device__ __forceinline__ bool second() const { return !BOTH && w >= PIECES; }
+  __device__ __forceinline__ unsigned offset(int i, int lane, int rs, int last) const {
+    const int p = (BOTH ? w : w % PIECES) * 64 + lane, row = p / CPR + STEP * i;
+    return __umul24(min(row, last), 2 * rs) + (((p % CPR) ^ swz(row)) << 4);
   }
-  __device__ __forceinline__ void one(const bf16* tile, int rs, int last, unsigned lds) const {
+  __device__ __forceinline__ void init(const char* smem, int w_, int64_t rsa_, int64_t rsb_) {
+    const int lane = threadIdx.x & 63;
+    w = w_;
+    lds = lds_addr(smem) + (BOTH ? w : w % PIECES) * 1024 + (second() ? TILE : 0);
+    rsa = (int)rsa_;
+    rsb = (int)rsb_;
+    if constexpr (TIGHT) {
+      chunk = offset(0, lane, 0, 31);
+      va[0] = offset(0, lane, rsa, 31) - chunk;
+      vb[0] = offset(0, lane, rsb, 31) - chunk;
+      return;
+    }
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      dma16(tile, __umul24(min(row + STEP * i, (unsigned)last), 2u * rs) + chunk[i], lds + at + i * W * 1024);
+    for (int i = 0; i < (TIGHT ? 1 : N); ++i) {
+      va[i] = offset(i, lane, second() ? rsb : rsa, 31);
+      if constexpr (BOTH) vb[i] = offset(i, lane, rsb, 31);
+    }
   }
-  // tile a to lds, tile b behind it
-  __device__ __forceinline__ void pair(const bf16* a, int64_t rsa, const bf16* b, int64_t rsb, int last, char* lds) const {
-    const unsigned dst = lds_addr(lds);
-    if constexpr (BOTH) {
-      one(a, (int)rsa, last, dst);
-      one(b, (int)rsb, last, dst + TileGeom<D>::TILE);
+  // tile a to byte OFF of the work group's LDS, tile b behind it
+  template <int OFF> __device__ __forceinline__ void pair(const bf16* a, const bf16* b) const {
+    if constexpr (TIGHT) {
+      dma16_at<OFF>(a, va[0] + chunk, lds);
+      dma16_at<OFF + TILE>(b, vb[0] + chunk, lds);
+      const unsigned c1 = chunk ^ 0x70;
+      dma16_at<OFF + W * 1024>(a, va[0] + c1 + 32 * rsa, lds);
+      dma16_at<OFF + TILE + W * 1024>(b, vb[0] + c1 + 32 * rsb, lds);
+    } else if constexpr (BOTH) {
+      unroll<N>([&](auto i) __attribute__((always_inline)) {
+        dma16_at<OFF + decltype(i)::value * W * 1024>(a, va[decltype(i)::value], lds);
+        dma16_at<OFF + TILE + decltype(i)::value * W * 1024>(b, vb[decltype(i)::value], lds);
+      });
     } else {
-      one(second ? b : a, (int)(second ? rsb : rsa), last, dst + (second ? TileGeom<D>::TILE : 0));
+      dma16_at<OFF>(second() ? b : a, va[0], lds);
+    }
+  }
+  template <int OFF> __device__ __forceinline__ void pair_last(const bf16* a, const bf16* b, int last) const {
+    const int lane = opaque(threadIdx.x & 63);
+    if constexpr (BOTH) {
+      unroll<N>([&](auto i) __attribute__((always_inline)) {
+        dma16_at<OFF + decltype(i)::value * W * 1024>(a, offset(decltype(i)::value, lane, rsa, last), lds);
+        dma16_at<OFF + TILE + decltype(i)::value * W * 1024>(b, offset(decltype(i)::value, lane, rsb, last), lds);
+      });
+    } else {
+      dma16_at<OFF>(second() ? b : a, offset(0, lane, second() ? rsb : rsa, last), lds);
+    }
+  }
+};
+
+// The key and value tiles of a work group, copied in order: a running pointer to
+// each, moved by a tile's rows, and once from the sinks to the window.
+template <int D, int W> struct KeyStream {
+  SwaCopy<D, W> tc;
+  const bf16 *k, *v;
+  int64_t dk, dv, jump_k, jump_v;
+  int x, n, sink_tiles, last;  // next tile; `last`: the last row of the last tile, below 31 if that is ragged
+  __device__ __forceinline__ void init(const SwaArgs& a, const KeyTiles& kt, int b, int hk, int len, const char* smem, int w) {
+    tc.init(smem, w, a.sk.s, a.sv.s);
+    dk = 32 * a.sk.s;
+    dv = 32 * a.sv.s;
+    jump_k = (kt.first - kt.sink_tiles) * dk;
+    jump_v = (kt.first - kt.sink_tiles) * dv;
+    k = (const bf16*)a.k + b * a.sk.b + hk * a.sk.h;
+    v = (const bf16*)a.v + b * a.sv.b + hk * a.sv.h;
+    x = 0;
+    n = kt.n;
+    sink_tiles = kt.sink_tiles;
+    if (sink_tiles == 0) {
+      k += jump_k;
+      v += jump_v;
+    }
+    last = min(31, len - 1 - kt.tile(n - 1) * 32);
+  }
+  // the next tile to byte OFF of the work group's LDS (after the last one: that again)
+  template <int OFF> __device__ __forceinline__ void copy() {
+    if (x < n - 1 || last == 31) tc.template pair<OFF>(k, v);
+    else tc.template pair_last<OFF>(k, v, last);
+    if (x >= n - 1) return;
+    ++x;
+    k += dk;
+    v += dv;
+    if (x == sink_tiles) {
+      k += jump_k;
+      v += jump_v;
     }
   }
 };
@@ -146,20 +229,14 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qg = w % QG, part = w / QG;
   const int BH = a.B * a.Hq, n_qtiles = (a.S + BQ - 1) / BQ;
-  const int bh = swa_head(blockIdx.x % BH, BH), qt = n_qtiles - 1 - blockIdx.x / BH;
-  const int b = bh / a.Hq, hq = bh - b * a.Hq, hk = hq / (a.Hq / a.Hkv);
+  const int bh = uniform(swa_head(blockIdx.x % BH, BH, a.Hq / a.Hkv)), qt = uniform(n_qtiles - 1 - blockIdx.x / BH);
+  const int b = uniform(bh / a.Hq), hq = bh - b * a.Hq, hk = uniform(hq / (a.Hq / a.Hkv));
   const int len = swa_len(a.lens, b, a.S);
   const int q0 = qt * BQ, qw = q0 + 32 * qg, my_q = qw + r;
   // (pointers from an opaque copy of the row, formed where they are used: kept
   // from here they would take registers across the loop)
-  auto out_row = [&](int q) {
-    asm volatile("" : "+v"(q));
-    return (bf16*)a.out + b * a.so.b + hq * a.so.h + q * a.so.s;
-  };
-  auto put_lse = [&](int q, float v) {
-    asm volatile("" : "+v"(q));
-    a.lse[(int64_t)bh * a.S + q] = v;
-  };
+  auto out_row = [&](int q) { return (bf16*)a.out + b * a.so.b + hq * a.so.h + opaque(q) * a.so.s; };
+  auto put_lse = [&](int q, float v) { a.lse[(int64_t)bh * a.S + opaque(q)] = v; };
   auto empty_row = [&] {  // this wave's share of a row without keys
     if (my_q >= a.S || my_q < len) return;
     bf16* orow = out_row(my_q);
@@ -176,17 +253,10 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
 
   const KeyTiles kt(q0, min(len, q0 + BQ), a.window, a.sinks);
   const int L = (kt.n + SPLIT - 1) / SPLIT;
-  const bf16* Kb = (const bf16*)a.k + b * a.sk.b + hk * a.sk.h;
-  const bf16* Vb = (const bf16*)a.v + b * a.sv.b + hk * a.sv.h;
-  SwaCopy<D, W> tc;
-  tc.init(w, lane);
-  auto dma = [&](int x, auto slc) {  // iteration x's tile of every part (without one: the last again)
-#pragma unroll
-    for (int p = 0; p < SPLIT; ++p) {
-      const int row0 = kt.tile(min(x * SPLIT + p, kt.n - 1)) * 32, last = min(31, len - 1 - row0);
-      char* dst = smem + (p * NB + decltype(slc)::value) * SET;
-      tc.pair(Kb + row0 * a.sk.s, a.sk.s, Vb + row0 * a.sv.s, a.sv.s, last, dst);
-    }
+  KeyStream<D, W> keys;
+  keys.init(a, kt, b, hk, len, smem, w);
+  auto dma = [&](int, auto slc) __attribute__((always_inline)) {  // the next iteration's tile of every part
+    unroll<SPLIT>([&](auto p) __attribute__((always_inline)) { keys.template copy<(decltype(p)::value * NB + decltype(slc)::value) * SET>(); });
   };
   constexpr int GROUP = ring_group(1, NB, 0, 2);
   ring_prologue<NB, GROUP>(L, dma);
@@ -198,6 +268,7 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   __syncthreads();
 
   const char* ring = smem + part * NB * SET;
+  const WaveTiles wt(kt, qw, len, a.window);
   float m = kMasked, lsum = 0.f;
   f32x16 oacc[DT];
 #pragma unroll
@@ -210,9 +281,7 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
       if (i >= L) return;
       ring_step<NB, GROUP, 0, 1, PER_SLOT, sl>(i, L, dma);
       const int x = i * SPLIT + part;
-      if (x >= kt.n || qw >= len) return;  // wave-uniform: nothing here, only the barriers
-      const int k0 = kt.tile(x) * 32;
-      if (!swa_tile_seen(qw, k0, a.window, a.sinks)) return;
+      if (!wt.seen(x)) return;  // wave-uniform: nothing here, only the barriers
       const char* t = ring + sl * SET;
       f32x16 s = f32x16{};
       MB::frag ka[2];
@@ -222,10 +291,11 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
         if (ks + 1 < KS_D) ka[(ks + 1) & 1] = fr.row(t, ks + 1);
         s = MB::run(ka[ks & 1], qf[ks], s);
       }
-      if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
+      if (wt.masked(x)) {
+        const int key = kt.tile(x) * 32 + 4 * opaque(h);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
+          s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
       }
       f32x16 pv;
       float psum = block_exp(s, c, m * c, pv);
@@ -350,17 +420,14 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qg = w % QG, part = w / QG;
   const int BH = a.B * a.Hq, n_qtiles = (a.S + BQ - 1) / BQ;
-  const int bh = swa_head(blockIdx.x % BH, BH), qt = n_qtiles - 1 - blockIdx.x / BH;
-  const int b = bh / a.Hq, hq = bh - b * a.Hq, hk = hq / (a.Hq / a.Hkv);
+  const int bh = uniform(swa_head(blockIdx.x % BH, BH, a.Hq / a.Hkv)), qt = uniform(n_qtiles - 1 - blockIdx.x / BH);
+  const int b = uniform(bh / a.Hq), hq = bh - b * a.Hq, hk = uniform(hq / (a.Hq / a.Hkv));
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int q0 = qt * BQ, qw = q0 + 32 * qg, my_q = qw + r;
   float* wsh = a.ws + (int64_t)bh * 2 * Sp;
   // (from an opaque copy of the row: kept from here, a pointer would take two
   // registers across the loop)
-  auto out_row = [&](int q) {
-    asm volatile("" : "+v"(q));
-    return (bf16*)a.dq + b * a.sdq.b + hq * a.sdq.h + q * a.sdq.s;
-  };
+  auto out_row = [&](int q) { return (bf16*)a.dq + b * a.sdq.b + hq * a.sdq.h + opaque(q) * a.sdq.s; };
   if (q0 >= len) {  // (no work group reads this one's workspace rows)
     bf16* row = out_row(my_q);
     if (part == 0 && my_q < a.S)
@@ -373,17 +440,10 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
 
   const KeyTiles kt(q0, min(len, q0 + BQ), a.window, a.sinks);
   const int L = (kt.n + SPLIT - 1) / SPLIT;
-  const bf16* Kb = (const bf16*)a.k + b * a.sk.b + hk * a.sk.h;
-  const bf16* Vb = (const bf16*)a.v + b * a.sv.b + hk * a.sv.h;
-  SwaCopy<D, W> tc;
-  tc.init(w, lane);
-  auto dma = [&](int x, auto slc) {
-#pragma unroll
-    for (int p = 0; p < SPLIT; ++p) {
-      const int row0 = kt.tile(min(x * SPLIT + p, kt.n - 1)) * 32, last = min(31, len - 1 - row0);
-      char* dst = smem + (p * NB + decltype(slc)::value) * SET;
-      tc.pair(Kb + row0 * a.sk.s, a.sk.s, Vb + row0 * a.sv.s, a.sv.s, last, dst);
-    }
+  KeyStream<D, W> keys;
+  keys.init(a, kt, b, hk, len, smem, w);
+  auto dma = [&](int, auto slc) __attribute__((always_inline)) {  // the next iteration's tile of every part
+    unroll<SPLIT>([&](auto p) __attribute__((always_inline)) { keys.template copy<(decltype(p)::value * NB + decltype(slc)::value) * SET>(); });
   };
   constexpr int GROUP = ring_group(1, NB, 0, 2);
   ring_prologue<NB, GROUP>(L, dma);
@@ -413,6 +473,7 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
   for (int ks = 0; ks < KS_D; ++ks) dof[ks] = negated(dof[ks]);
 
   const char* ring = smem + part * NB * SET;
+  const WaveTiles wt(kt, qw, len, a.window);
   f32x16 acc[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
@@ -424,9 +485,7 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
       if (i >= L) return;
       ring_step<NB, GROUP, 0, 1, PER_SLOT, sl>(i, L, dma);
       const int x = i * SPLIT + part;
-      if (x >= kt.n || qw >= len) return;
-      const int k0 = kt.tile(x) * 32;
-      if (!swa_tile_seen(qw, k0, a.window, a.sinks)) return;
+      if (!wt.seen(x)) return;
       const char* t = ring + sl * SET;
       // D broadcast into the accumulator here, not kept in 16 registers across the loop
       float d = Dq;
@@ -446,10 +505,11 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
         s = MB::run(ka[ks & 1], qf[ks], s);
         dx = MB::run(va[ks & 1], dof[ks], dx);  // D - dP^T
       }
-      if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
+      if (wt.masked(x)) {
+        const int key = kt.tile(x) * 32 + 4 * opaque(h);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
+          s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) dx[e] = -exp2_hw(fmaf(s[e], c, -lse2)) * dx[e];  // dS^T = P (dP - D)
@@ -491,9 +551,9 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = w % KG, part = w / KG;
   const int BH = a.B * a.Hkv, group = a.Hq / a.Hkv;
-  const int bkv = swa_head(blockIdx.x % BH, BH), rest = blockIdx.x / BH;
-  const int chunk = FAR ? rest % far_parts : 0, kt = FAR ? rest / far_parts : rest;
-  const int b = bkv / a.Hkv, hk = bkv - b * a.Hkv;
+  const int bkv = uniform(blockIdx.x % BH), rest = uniform(blockIdx.x / BH);
+  const int chunk = FAR ? uniform(rest % far_parts) : 0, kt = FAR ? uniform(rest / far_parts) : rest;
+  const int b = uniform(bkv / a.Hkv), hk = bkv - b * a.Hkv;
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int k0 = kt * BKV, kw = k0 + 32 * kg, my_k = kw + r;
   const bool far = FAR || swa_has_far(true, a.Hq, a.Hkv, a.S, a.window, a.sinks);  // sink keys' sums go to the far area
@@ -511,36 +571,53 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   }
   const int L = (n + SPLIT - 1) / SPLIT;
 
-  SwaCopy<D, W> tc;
-  tc.init(w, lane);
-  const bf16* Qb = (const bf16*)a.q + b * a.sq.b + (int64_t)hk * group * a.sq.h;
-  const bf16* dOb = (const bf16*)a.dout + b * a.sdo.b + (int64_t)hk * group * a.sdo.h;
-  const float* wsb = a.ws + ((int64_t)b * a.Hq + hk * group) * 2 * Sp;
+  SwaCopy<D, W, D == 128 && W == 4> tc;
+  tc.init(smem, w, a.sq.s, a.sdo.s);
   // a part's 8 chunks of -LSE/scale and 8 of D: lanes 0..3 of four waves
   const int ldq = 4 * (w & 3) + (lane & 3);
   const unsigned ld_voff = (unsigned)((ldq < 8 ? Sp + 4 * ldq : 4 * (ldq - 8)) * 4);
-  // the walk: position x is query tile jhi - x % nj of head x / nj
-  int head = n ? x0 / nj : 0, j = n ? jhi - x0 % nj : 0;  // next position to copy
-  int jc = j;                                             // this wave's next position
-  auto dma = [&](int x, auto slc) {
-#pragma unroll
-    for (int p = 0; p < SPLIT; ++p) {
-      const int row0 = j * 32, last = min(31, len - 1 - row0);
-      char* dst = smem + (p * NB + decltype(slc)::value) * SETB;
-      tc.pair(Qb + head * a.sq.h + row0 * a.sq.s, a.sq.s, dOb + head * a.sdo.h + row0 * a.sdo.s, a.sdo.s, last, dst);
-      if ((W == 4 || w / 4 == p) && lane < 4)
-        dma16(wsb + (int64_t)head * 2 * Sp + row0, ld_voff,
-              lds_addr(smem + AUX0 + (p * NB + decltype(slc)::value) * AUX) + 64 * (w & 3));
-      if (x * SPLIT + p + 1 < n && --j < jlo) {  // (a part without a tile copies the last again)
+  // The walk: position x is query tile jhi - x % nj of head x / nj.  Running
+  // pointers to the next position to copy, moved up a tile, or to the last tile
+  // of the next head.
+  const int head0 = uniform(n ? x0 / nj : 0);
+  int j = n ? jhi - (x0 - head0 * nj) : 0, pos = 0;
+  int jc = j;  // this wave's next position
+  const int64_t row0 = j * 32, back = nj * 32;
+  const bf16* qp = (const bf16*)a.q + b * a.sq.b + ((int64_t)hk * group + head0) * a.sq.h + row0 * a.sq.s;
+  const bf16* dop = (const bf16*)a.dout + b * a.sdo.b + ((int64_t)hk * group + head0) * a.sdo.h + row0 * a.sdo.s;
+  const float* wsp = a.ws + ((int64_t)b * a.Hq + hk * group + head0) * 2 * Sp + row0;
+  const int64_t up_q = 32 * a.sq.s, up_do = 32 * a.sdo.s;
+  const int64_t next_q = a.sq.h + back * a.sq.s, next_do = a.sdo.h + back * a.sdo.s, next_ws = 2 * (int64_t)Sp + back;
+  const int jrag = len % 32 ? len / 32 : -1;  // the tile that reaches past the end
+  const unsigned aux_lds = lds_addr(smem) + 64 * (w & 3);
+  auto dma = [&](int, auto slc) __attribute__((always_inline)) {
+    unroll<SPLIT>([&](auto p_) __attribute__((always_inline)) {
+      constexpr int p = decltype(p_)::value, slot = p * NB + decltype(slc)::value;
+      if (j != jrag) tc.template pair<slot * SETB>(qp, dop);
+      else tc.template pair_last<slot * SETB>(qp, dop, len % 32 - 1);
+      if ((W == 4 || w / 4 == p) && lane < 4) dma16_at<AUX0 + slot * AUX>(wsp, ld_voff, aux_lds);
+      if (SPLIT > 1 && ++pos >= n) return;  // (a part without a tile copies the last again)
+      qp -= up_q;
+      dop -= up_do;
+      wsp -= 32;
+      if (--j < jlo) {
         j = jhi;
-        ++head;
+        qp += next_q;
+        dop += next_do;
+        wsp += next_ws;
       }
-    }
+    });
   };
   auto advance = [&](int& at, int by) {
     at -= by;
     while (at < jlo) at += nj;
   };
+  // this wave's tiles: [wlo, whi] hold pairs that count, those up to wdiag and
+  // from wedge on hidden ones too (FAR: those below wedge, or all)
+  const int wlo = FAR ? (max(kw + a.window - 31, 0) + 31) / 32 : kw / 32;
+  const int whi = FAR || kw < sinks ? jhi : kw < len ? (kw + 31 + a.window - 1) / 32 : -1;
+  const int wdiag = FAR ? (kw + 32 > a.sinks ? jhi : -1) : kw / 32;
+  const int wedge = FAR ? (kw + 31 + a.window + 31) / 32 : (max(kw + a.window - 31, 0) + 31) / 32;
   constexpr int GROUP = ring_group(1, NB, 0, 2);
   ring_prologue<NB, GROUP>(L, dma);
   if (n) advance(jc, part);
@@ -570,11 +647,9 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
       if (i >= L) return;
       ring_step<NB, GROUP, 0, 1, PER_SLOT, sl>(i, L, dma);
       if (i * SPLIT + part >= n) return;
-      const int qs = jc * 32;
+      const int jw = jc;
       advance(jc, SPLIT);
-      if (FAR ? qs + 31 - kw < a.window
-              : kw >= len || qs + 31 < kw || (qs - (kw + 31) >= a.window && kw >= sinks))
-        return;
+      if (jw < wlo || jw > whi) return;
       const char* lq = ring + sl * SETB;
       const char* ldo = lq + TILE;
       const float* llse = (const float*)(aux + sl * AUX);
@@ -602,17 +677,16 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
         s = MB::run(qa[ks & 1], kf[ks], s);
         dx = MB::run(da[ks & 1], vf[ks], dx);  // D - dP
       }
-      // s[e], dx[e]: S - LSE/scale and D - dP of query qs + acc_row(e, h), key my_k
-      const bool masked = FAR ? qs - (kw + 31) < a.window || kw + 32 > a.sinks : qs < kw + 31 || qs + 31 - kw >= a.window;
-      if (masked || qs + 32 > len) {
-        int key = my_k;
-        asm volatile("" : "+v"(key));  // (what follows is not hoisted out of the rare branch into registers)
+      // s[e], dx[e]: S - LSE/scale and D - dP of query 32 jw + acc_row(e, h), key my_k
+      if (jw <= wdiag || (FAR ? jw < wedge : jw >= wedge) || jw == jrag) {
+        const int qs = jw * 32;
+        const int key = opaque(my_k), qry = qs + 4 * opaque(h);
         const int low = FAR ? a.window : 0;  // the pair counts where low <= query - key < high
         const int high = FAR ? (key < a.sinks ? INT_MAX : 0) : key < sinks ? INT_MAX : a.window;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int qry = qs + acc_row(e, h), ahead = qry - key;
-          s[e] = swa_masked((ahead >= low) & (ahead < high) & (qry < len), s[e]);
+          const int q = qry + acc_row(e, 0), ahead = q - key;
+          s[e] = swa_masked((ahead >= low) & (ahead < high) & (q < len), s[e]);
         }
       }
 #pragma unroll
@@ -643,8 +717,7 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
 
   if constexpr (SPLIT > 1) wait_vm(0);
   const int dim = D;
-  int key = my_k;
-  asm volatile("" : "+v"(key));  // (no pointers kept across the loop)
+  const int key = opaque(my_k);  // (no pointers kept across the loop)
   bf16* krow = (bf16*)a.dk + b * a.sdk.b + hk * a.sdk.h + key * a.sdk.s;
   bf16* vrow = (bf16*)a.dv + b * a.sdv.b + hk * a.sdv.h + key * a.sdv.s;
   auto put = [&](bf16* out, int which, float f, int col, const f32x4& v) {

@@ -10,14 +10,31 @@
 
 namespace cattn {
 
+// A value that is the same in every lane, into a scalar register (the compiler
+// leaves what a division gives in vector ones, and all that follows from it).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// x, by a way the compiler cannot see through: what is formed from it in a rare
+// branch is not formed before the loop and kept in registers.
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Tokens of sequence b.
 __device__ __forceinline__ int swa_len(const int* lens, int b, int S) { return lens ? min(max(lens[b], 0), S) : S; }
 
-// The i-th head of n in the order work groups take them: with n a multiple of
-// 8, work group i runs on chiplet i % 8, and each chiplet takes n / 8
-// consecutive heads, so that the query heads of a key/value head share its
-// tiles in one L2.
-__device__ __forceinline__ int swa_head(int i, int n) { return n % 8 == 0 ? (i & 7) * (n >> 3) + (i >> 3) : i; }
+// The i-th query head of n in the order work groups take them.  Work group i runs
+// on chiplet i % 8.  With a multiple of 8 key/value heads, each chiplet takes every
+// eighth of them, with all its query heads (which share its tiles in one L2): the
+// heads of one sequence, which in a padded batch may be short, are then spread
+// over the chiplets (B8 H12 S1024 D64, lengths 512 .. 1024, window 256, forward and
+// backward: 65.4 -> 62.9 us against a sequence per chiplet).  With fewer, n / 8
+// consecutive heads.
+__device__ __forceinline__ int swa_head(int i, int n, int group) {
+  if (n / group % 8 == 0) return (i & 7) * group + (i >> 3) / group * 8 * group + (i >> 3) % group;
+  return n % 8 == 0 ? (i & 7) * (n >> 3) + (i >> 3) : i;
+}
 
 // Masks are selects of conditions joined by & and |.  With && and || the compiler
 // (ROCm 7.2's) made branches of them, and in one kernel lost the assignment of an
@@ -31,20 +48,37 @@ __device__ __forceinline__ float swa_masked(bool seen, float score) { return see
 // then first .. first + n - sink_tiles - 1.
 struct KeyTiles {
   int sink_tiles, first, n;
+  int with_sinks;  // indexes below hold sinks, wherever the window begins
   __device__ __forceinline__ KeyTiles(int q0, int q1, int window, int sinks) {
     const int last = (q1 - 1) / 32;
     first = max(q0 - window + 1, 0) / 32;
-    sink_tiles = min((min(sinks, q1) + 31) / 32, first);
+    with_sinks = (min(sinks, q1) + 31) / 32;
+    sink_tiles = min(with_sinks, first);
     n = sink_tiles + last - first + 1;
   }
   __device__ __forceinline__ int tile(int x) const { return x < sink_tiles ? x : x - sink_tiles + first; }
 };
 
-// Whether queries [q, q + 32) see any key of the tile at k0, and whether any
-// pair of the two is hidden.
-__device__ __forceinline__ bool swa_tile_seen(int q, int k0, int window, int sinks) {
-  return k0 <= q + 31 && (q - (k0 + 31) < window || k0 < sinks);
-}
+// Of a work group's tiles, by index x: which a wave with queries [q, q + 32) below
+// `len` sees any key of (those with sinks, and [lo, hi]), and which hold a pair
+// that is hidden (below edge: outside the window of some query, the sinks' tiles
+// before the window with them; from diag on: the diagonal).  Compares against
+// indexes formed once.
+struct WaveTiles {
+  int with_sinks, lo, hi, edge, diag;
+  __device__ __forceinline__ WaveTiles(const KeyTiles& kt, int q, int len, int window) {
+    const int shift = kt.sink_tiles - kt.first;
+    with_sinks = kt.with_sinks;
+    lo = max(q - window + 1, 0) / 32 + shift;
+    hi = q < len ? (min(q + 32, len) - 1) / 32 + shift : -1;
+    edge = (max(q + 32 - window, 0) + 31) / 32 + shift;
+    diag = q / 32 + shift;
+  }
+  __device__ __forceinline__ bool seen(int x) const { return x <= hi && (x >= lo || x < with_sinks); }
+  __device__ __forceinline__ bool masked(int x) const { return x < edge || x >= diag; }
+};
+
+// Whether any pair of queries [q, q + 32) and the tile at k0 is hidden.
 __device__ __forceinline__ bool swa_tile_masked(int q, int k0, int window, int sinks) {
   return k0 + 31 > q || (q + 31 - k0 >= window && k0 + 32 > sinks);
 }

@@ -36,18 +36,12 @@ void swa_fwd_f32_kernel(SwaArgs a, float c) {
   const Lanes l_;
   const int lane = l_.lane, h = l_.h, r = l_.r, w = l_.w;
   const int BH = a.B * a.Hq, n_qtiles = (a.S + 31) / 32;
-  const int bh = swa_head(blockIdx.x % BH, BH), qt = n_qtiles - 1 - blockIdx.x / BH;
+  const int bh = swa_head(blockIdx.x % BH, BH, a.Hq / a.Hkv), qt = n_qtiles - 1 - blockIdx.x / BH;
   const int b = bh / a.Hq, hq = bh - b * a.Hq, hk = hq / (a.Hq / a.Hkv);
   const int len = swa_len(a.lens, b, a.S), qw = qt * 32, my_q = qw + r;
   // (pointers from an opaque copy of the row, formed where they are used)
-  auto out_row = [&](int q) {
-    asm volatile("" : "+v"(q));
-    return (float*)a.out + b * a.so.b + hq * a.so.h + q * a.so.s;
-  };
-  auto put_lse = [&](int q, float v) {
-    asm volatile("" : "+v"(q));
-    a.lse[(int64_t)bh * a.S + q] = v;
-  };
+  auto out_row = [&](int q) { return (float*)a.out + b * a.so.b + hq * a.so.h + opaque(q) * a.so.s; };
+  auto put_lse = [&](int q, float v) { a.lse[(int64_t)bh * a.S + opaque(q)] = v; };
   if (w == 0 && my_q >= len && my_q < a.S) {  // a row without keys
     const ColBlocks<D> zero{};
     float* orow = out_row(my_q);
@@ -76,9 +70,10 @@ void swa_fwd_f32_kernel(SwaArgs a, float c) {
     typename G::TransFrags vt;
     f32x16 s = contract_rows<D, 16>(kr, sm, lane, f32x16{}, [&](int e) { vt[e] = Vm.trans_step(k0, e); });
     if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
+      const int key = k0 + 4 * opaque(h);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
+        s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
     }
     float mx = s[0];
 #pragma unroll
@@ -159,7 +154,7 @@ void swa_dq_f32_kernel(SwaArgs a, float c) {
   const Lanes l_;
   const int lane = l_.lane, h = l_.h, r = l_.r, w = l_.w;
   const int BH = a.B * a.Hq, n_qtiles = (a.S + 31) / 32;
-  const int bh = swa_head(blockIdx.x % BH, BH), qt = n_qtiles - 1 - blockIdx.x / BH;
+  const int bh = swa_head(blockIdx.x % BH, BH, a.Hq / a.Hkv), qt = n_qtiles - 1 - blockIdx.x / BH;
   const int b = bh / a.Hq, hq = bh - b * a.Hq, hk = hq / (a.Hq / a.Hkv);
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S), qw = qt * 32, my_q = qw + r;
   float* row = (float*)a.dq + b * a.sdq.b + hq * a.sdq.h + my_q * a.sdq.s;
@@ -211,9 +206,10 @@ void swa_dq_f32_kernel(SwaArgs a, float c) {
     f32x16 s = contract_rows<D, G::KJ>(kr, qf, lane, f32x16{}, [&](int j) { vr[j] = row_chunk(vp, j); });
     f32x16 dp = contract_rows<D, 16>(vr, dof, lane, f32x16{}, [&](int e) { ktr[e] = Km.trans_step(k0, e); });
     if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
+      const int key = k0 + 4 * opaque(h);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        s[e] = swa_masked(swa_sees(my_q, k0 + acc_row(e, h), a.window, a.sinks), s[e]);
+        s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = exp2_hw(fmaf(s[e], c, -lse2)) * (dp[e] - Dq);  // dS^T
@@ -234,7 +230,7 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
   const Lanes l_;
   const int lane = l_.lane, h = l_.h, r = l_.r, w = l_.w;
   const int BH = a.B * a.Hkv, group = a.Hq / a.Hkv;
-  const int bkv = swa_head(blockIdx.x % BH, BH), rest = blockIdx.x / BH;
+  const int bkv = blockIdx.x % BH, rest = blockIdx.x / BH;
   const int chunk = FAR ? rest % far_parts : 0, kt = FAR ? rest / far_parts : rest;
   const int b = bkv / a.Hkv, hk = bkv - b * a.Hkv;
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
@@ -309,12 +305,13 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
     f32x16 dp = contract_rows<D, 16>(dor, vf, lane, f32x16{}, [&](int e) { dot[e] = dOm.trans_step(q0, e); });
     const bool masked = FAR ? q0 - (kw + 31) < a.window || kw + 32 > a.sinks : q0 < kw + 31 || q0 + 31 - kw >= a.window;
     if (masked || q0 + 32 > len) {
+      const int key = opaque(my_k), qry = q0 + 4 * opaque(h);
       const int low = FAR ? a.window : 0;  // the pair counts where low <= query - key < high
-      const int high = FAR ? (my_k < a.sinks ? INT_MAX : 0) : my_k < sinks ? INT_MAX : a.window;
+      const int high = FAR ? (key < a.sinks ? INT_MAX : 0) : key < sinks ? INT_MAX : a.window;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int qry = q0 + acc_row(e, h), ahead = qry - my_k;
-        s[e] = swa_masked((ahead >= low) & (ahead < high) & (qry < len), s[e]);
+        const int q = qry + acc_row(e, 0), ahead = q - key;
+        s[e] = swa_masked((ahead >= low) & (ahead < high) & (q < len), s[e]);
       }
     }
 #pragma unroll
