@@ -410,6 +410,7 @@ cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const vo
   cattn_status st = swa_sizes(B, Hq, Hkv, S, D, window, sinks, scale, layout, dtype, &empty);
   if (st != CATTN_OK || empty) return st;
   if ((int64_t)(Hq / Hkv) * ((S + 31) / 32) > INT_MAX / 2) return fail(CATTN_ERR_UNSUPPORTED, "group too large");
+  if ((int64_t)B * Hkv * std::min(sinks, S) > INT_MAX) return fail(CATTN_ERR_UNSUPPORTED, "too many sinks");
   if (!q || !k || !v || !o || !dout || !lse || !dq || !dk || !dv || !workspace)
     return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");
   if (!aligned(lse, 4) || !aligned(lens, 4)) return fail(CATTN_ERR_INVALID_ARG, "lse and lens must be 4-byte aligned");
