@@ -183,7 +183,7 @@ cattn_status cattn_rmsnorm_fwd_q8(const void* x, const void* residual, const flo
 
 size_t cattn_rmsnorm_bwd_workspace_bytes(int rows, int C) {
   if (rows <= 0 || C <= 0) return 0;
-  return (size_t)rms_bwd_groups(rows) * (size_t)C * sizeof(float);
+  return (size_t)rms_bwd_groups(rows, C) * (size_t)C * sizeof(float);
 }
 
 cattn_status cattn_rmsnorm_bwd(const void* h, const float* gamma, const float* rstd, const void* dy, const void* dh,

@@ -34,12 +34,26 @@ struct RmsBwd {
   const void* dh;  // or NULL
   void* dx;
   float* dgamma;
-  float* part;  // rms_bwd_groups(rows) partial rows of dgamma
+  float* part;  // rms_bwd_groups(rows, C) partial rows of dgamma
   int rows, C;
   bool bf16;
 };
-// Work groups of the backward's first kernel; each leaves one partial row of dgamma.
-constexpr int rms_bwd_groups(int rows) { return rows <= 0 ? 0 : (rows + 7) / 8 < 512 ? (rows + 7) / 8 : 512; }
+// Waves that take a row of the backward: one up to 1024 columns, four up to 2048,
+// else 16.  (One / four / 16, us: 16384 x 768 20.3 / 30.7 / 49.8; 16384 x 2048
+// - / 42.8 / 52.0; 16384 x 4096 - / 107.6 / 106.0; 2048 x 4096 - / 16.8 / 16.5.)
+constexpr int rms_bwd_waves(int C) { return C <= 1024 ? 1 : C <= 2048 ? 4 : 16; }
+// Work groups of its first kernel, each with a block of rows; each leaves one
+// partial row of dgamma.  As many as there are rows at once, up to 256, since few
+// rows are the latency of one group's; beyond that eight rows a group, up to 512,
+// since every partial row is read again.  (Eight rows a group from the first on / as
+// many groups as rows, up to 512, us: 64 x 768 6.5 / 5.8, 64 x 4096 12.3 / 6.5, 512
+// x 4096 13.1 / 14.6, 2048 x 8192 27.7 / 31.8; by this rule 5.8, 6.5, 10.9, 27.5.)
+constexpr int rms_bwd_groups(int rows, int C) {
+  if (rows <= 0) return 0;
+  const int at_once = rms_bwd_waves(C) == 1 ? 4 : 1;  // rows of a work group
+  const int few = (rows - 1) / at_once + 1, many = (rows - 1) / 8 + 1;
+  return many >= 512 ? 512 : few <= 256 ? few : many > 256 ? many : 256;
+}
 hipError_t launch_rmsnorm_fwd(const RmsFwd& a, hipStream_t st);
 hipError_t launch_rmsnorm_bwd(const RmsBwd& a, hipStream_t st);
 

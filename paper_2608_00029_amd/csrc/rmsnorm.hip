@@ -323,17 +323,18 @@ __global__ __launch_bounds__(1024) void rmsnorm_bwd_sum_kernel(const float* __re
     ((f32x4*)dgamma)[q] = t;
   }
 }
-static_assert(rms_bwd_groups(1 << 30) == 512, "two partial rows per stream");
+static_assert(rms_bwd_groups(1 << 30, 8) == 512 && rms_bwd_groups(1 << 30, kRmsMaxC) == 512, "two partial rows per stream");
 
-// Waves per row and steps per lane: as many waves as keep a row at four steps
-// or fewer, and more where there are too few rows to fill the GPU with them
-// (latency: a step's loads are in flight together either way).
+// Waves per row of the forward: one up to 1024 columns, then four, and 16 above
+// 8192; more where there are too few rows to fill the GPU with them (a call is then
+// the latency of one row).  Measured with the residual, bf16, one / four / 16, us:
+//   rows x C   1 x 768 2.7 / 2.4;  1024 x 768 3.5 / 3.2;  2048 x 768 3.7 / 4.0;  16384 x 768 16.2 / 17.6;
+//              1024 x 512 2.9 / 3.3;  2048 x 1600 5.3 / 4.5;  16384 x 1600 33.3 / 32.1;
+//              64 x 4096 - / 3.3 / 2.9;  512 x 4096 - / 4.2 / 4.4;  512 x 8192 - / 5.8 / 5.1;  1024 x 8192 - / 9.9 / 10.3
 int rms_waves(int rows, int C) {
-  const int64_t oct = C / 8;
-  int w = oct <= 4 * 64 ? 1 : oct <= 16 * 64 ? 4 : 16;
-  if (w == 1 && oct > 64 && rows <= 4 * 256) w = 4;
-  if (w == 4 && oct > 4 * 64 && rows <= 256) w = 16;
-  return w;
+  if (C <= 1024) return C > 512 && rows <= 1024 ? 4 : 1;
+  if (C > 8192) return 16;
+  return C > 2048 && rows <= (C > 4096 ? 512 : 256) ? 16 : 4;
 }
 
 // f(steps), from the fewest to the most that W waves a row are taken with.
@@ -344,7 +345,7 @@ template <int W, int LO, int HI, typename F> hipError_t by_steps(int C, F&& f) {
   }
   return f(std::integral_constant<int, LO>{});
 }
-constexpr int most_steps(int W) { return W == 16 ? 2 : 4; }
+constexpr int most_steps(int W) { return W == 4 ? 4 : 2; }
 static_assert(kRmsMaxC / 8 <= most_steps(16) * 64 * 16, "16 waves hold the widest row");
 
 template <typename T, int W> hipError_t fwd_w(const RmsFwd& a, hipStream_t st) {
@@ -374,8 +375,8 @@ template <typename T> hipError_t fwd_t(const RmsFwd& a, hipStream_t st) {
 
 template <typename T, int W> hipError_t bwd_w(const RmsBwd& a, hipStream_t st) {
   constexpr int WG = W == 16 ? 16 : 4;
-  const dim3 grid((unsigned)rms_bwd_groups(a.rows)), block(WG * 64);
-  return by_steps<W, 1, 2>(a.C, [&](auto n) {
+  const dim3 grid((unsigned)rms_bwd_groups(a.rows, a.C)), block(WG * 64);
+  return by_steps<W, 1, W == 4 ? 1 : 2>(a.C, [&](auto n) {
     constexpr int N = decltype(n)::value;
     if (a.dh) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, W, N, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, W, N, false>), grid, block, 0, st, a);
@@ -384,11 +385,11 @@ template <typename T, int W> hipError_t bwd_w(const RmsBwd& a, hipStream_t st) {
 }
 
 template <typename T> hipError_t bwd_t(const RmsBwd& a, hipStream_t st) {
-  const int oct = a.C / 8;
-  hipError_t e = oct <= 2 * 64 ? bwd_w<T, 1>(a, st) : oct <= 8 * 64 ? bwd_w<T, 4>(a, st) : bwd_w<T, 16>(a, st);
+  const int w = rms_bwd_waves(a.C);
+  hipError_t e = w == 1 ? bwd_w<T, 1>(a, st) : w == 4 ? bwd_w<T, 4>(a, st) : bwd_w<T, 16>(a, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(rmsnorm_bwd_sum_kernel, dim3((unsigned)((a.C / 4 + 3) / 4)), dim3(1024), 0, st,
-                     (const float*)a.part, a.dgamma, rms_bwd_groups(a.rows), a.C);
+                     (const float*)a.part, a.dgamma, rms_bwd_groups(a.rows, a.C), a.C);
   return hipGetLastError();
 }
 

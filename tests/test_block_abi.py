@@ -142,7 +142,8 @@ def test_views_of_one_allocation_are_told_apart(lib):
 
 def test_workspace_sizes(lib):
     assert cattn.rmsnorm_bwd_workspace_bytes(10000, 64) == 512 * 64 * 4
-    assert cattn.rmsnorm_bwd_workspace_bytes(9, 64) == 2 * 64 * 4 and cattn.rmsnorm_bwd_workspace_bytes(0, 64) == 0
+    assert cattn.rmsnorm_bwd_workspace_bytes(9, 64) == 3 * 64 * 4 and cattn.rmsnorm_bwd_workspace_bytes(0, 64) == 0
+    assert cattn.rmsnorm_bwd_workspace_bytes(9, 4096) == 9 * 4096 * 4
     rows = 2 * 2 * 4 * 64 * 4
     assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 40, 64, 40, 2) == rows  # the window covers the sequence
     assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 40, 64, 8, 0) == rows   # no sinks

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 # rows x C: one row, one 8-column row, a row that ends inside a wave's step, each number of waves and
 # steps a row takes, more rows than work groups take at once, the widest row
 SHAPES = [(1, 8), (3, 64), (5, 520), (7, 1600), (2, 2048), (9, 2056), (1, 4096), (70, 4104), (3, 8192), (2, 8200),
-          (2, 16384), (300, 2056), (1030, 768), (1025, 1032), (8200, 128), (2100, 2560)]
+          (2, 16384), (300, 2056), (1030, 768), (1024, 1024), (1025, 1032), (8200, 128), (2100, 2560), (513, 8192), (600, 8200)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
