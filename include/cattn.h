@@ -440,8 +440,8 @@ cattn_status cattn_rope_append(const void* q, const void* k, const void* v, void
  *             -infinity.  (A value of a token itself that is not finite may reach
  *             rows that do not see it but share its 32-row tile.)
  *   workspace: at least cattn_swa_bwd_workspace_bytes(...) bytes, 16-byte aligned
- * Supported: D in {64, 128}; S <= 2^26; B * Hq * ceil(S / 32) < 2^31; window >=
- * 1, sinks >= 0; scale in [1e-20, 1e6]; tensors 16-byte aligned, with strides of
+ * Supported: D in {64, 128}; S <= 2^26; B * Hq * ceil(S / 32) < 2^24, in
+ * the backward B * Hkv * sinks too; window >= 1, sinks >= 0; scale in [1e-20, 1e6]; tensors 16-byte aligned, with strides of
  * whole 16 bytes and row strides below 2^23 elements.
  */
 cattn_status cattn_swa_fwd(const void* q, const void* k, const void* v, void* o, float* lse, const int* lens, int B,
@@ -472,7 +472,8 @@ size_t cattn_swa_bwd_workspace_bytes(int B, int Hq, int Hkv, int S, int D, int w
  *   lse:      out, float [B, Hq]
  *   workspace: at least cattn_swa_decode_workspace_bytes(...) bytes, 16-byte
  *             aligned; may be NULL where that is 0
- * Supported: as for cattn_swa_fwd, with cap <= 2^26 in place of S.
+ * Supported: as for cattn_swa_fwd, but cap <= 2^26 and B * Hq < 2^24 in place of
+ * the limits on S.
  */
 cattn_status cattn_swa_decode(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
                               const int* lens, float* workspace, int B, int Hq, int Hkv, int cap, int D, int window,

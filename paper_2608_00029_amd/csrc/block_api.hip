@@ -337,6 +337,9 @@ cattn_status cattn_rope_append(const void* q, const void* k, const void* v, void
 // ---------------------------------------------------------------------------
 // Sliding-window attention
 // ---------------------------------------------------------------------------
+// Work groups that a launch may have: their threads (256 each) are counted in 32 bits.
+constexpr int64_t kMaxGroups = 1 << 24;
+
 static cattn_status swa_sizes(int B, int Hq, int Hkv, int S, int D, int window, int sinks, float scale, int layout,
                               int dtype, bool* empty) {
   *empty = false;
@@ -353,8 +356,7 @@ static cattn_status swa_sizes(int B, int Hq, int Hkv, int S, int D, int window, 
   }
   if (Hq == 0 || Hkv == 0 || Hq % Hkv) return fail(CATTN_ERR_INVALID_ARG, "Hq must be a multiple of Hkv");
   if (S > (1 << 26)) return fail(CATTN_ERR_UNSUPPORTED, "S (cap) exceeds 2^26");
-  if ((int64_t)B * Hq > INT_MAX || (int64_t)B * Hq * ((S + 31) / 32) > INT_MAX)
-    return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
+  if ((int64_t)B * Hq >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
   return CATTN_OK;
 }
 
@@ -374,6 +376,7 @@ cattn_status cattn_swa_fwd(const void* q, const void* k, const void* v, void* o,
   bool empty;
   cattn_status st = swa_sizes(B, Hq, Hkv, S, D, window, sinks, scale, layout, dtype, &empty);
   if (st != CATTN_OK || empty) return st;
+  if ((int64_t)B * Hq * ((S + 31) / 32) >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
   if (!q || !k || !v || !o || !lse) return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");
   if (!aligned(lse, 4) || !aligned(lens, 4)) return fail(CATTN_ERR_INVALID_ARG, "lse and lens must be 4-byte aligned");
   const size_t esz = dtype == CATTN_BF16 ? 2 : 4;
@@ -409,8 +412,8 @@ cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const vo
   bool empty;
   cattn_status st = swa_sizes(B, Hq, Hkv, S, D, window, sinks, scale, layout, dtype, &empty);
   if (st != CATTN_OK || empty) return st;
-  if ((int64_t)(Hq / Hkv) * ((S + 31) / 32) > INT_MAX / 2) return fail(CATTN_ERR_UNSUPPORTED, "group too large");
-  if ((int64_t)B * Hkv * std::min(sinks, S) > INT_MAX) return fail(CATTN_ERR_UNSUPPORTED, "too many sinks");
+  if ((int64_t)B * Hq * ((S + 31) / 32) >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
+  if ((int64_t)B * Hkv * std::min(sinks, S) >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "too many sinks");
   if (!q || !k || !v || !o || !dout || !lse || !dq || !dk || !dv || !workspace)
     return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");
   if (!aligned(lse, 4) || !aligned(lens, 4)) return fail(CATTN_ERR_INVALID_ARG, "lse and lens must be 4-byte aligned");

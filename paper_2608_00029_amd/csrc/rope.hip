@@ -78,14 +78,15 @@ __device__ __forceinline__ int cache_slot(int p, int len, const RopeArgs& a) {
 
 // Items of a head's row: the rotated part in steps of V pairs (half layout) or
 // V / 2 pairs (interleaved), then the rest in steps of V columns.  A row is one
-// head of one token; the work groups (x, y), y = 0 .. gridDim.y - 1, share the
+// head of one token; the work groups (x, y, z), y = 0 .. gridDim.y - 1, share the
 // rows of their tokens.
 template <typename T, int V, bool INTER, bool APPEND>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int tpg, int items, int rot_items) {
   __shared__ float cs[kRopeTable], sn[kRopeTable];
   __shared__ Token tok[kMaxTokens];
   const int tid = threadIdx.x, half = a.rot >> 1;
-  const int64_t total = (int64_t)a.B * a.S, first = (int64_t)blockIdx.x * tpg;
+  const int64_t total = (int64_t)a.B * a.S, first = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * tpg;
+  if (first >= total) return;
   const int n_tok = (int)(total - first < tpg ? total - first : tpg);
 
   auto place = [&](int t, Token& k) {  // token t of this work group; returns its position
@@ -236,7 +237,10 @@ template <typename T, int V, bool INTER> hipError_t rope_v(const RopeArgs& a, hi
   const int64_t passes = ((int64_t)tpg * (a.Hq + a.Hkv) * items + 255) / 256;
   int64_t shares = 2 * cu_count() / groups;
   shares = shares < 1 ? 1 : shares < passes ? shares : passes;
-  const dim3 grid((unsigned)groups, (unsigned)shares);
+  // (a launch counts the threads of each grid dimension in 32 bits)
+  constexpr int64_t kMaxX = 1 << 23;
+  const int64_t z = (groups + kMaxX - 1) / kMaxX;
+  const dim3 grid((unsigned)((groups + z - 1) / z), (unsigned)shares, (unsigned)z);
   if (a.append) hipLaunchKernelGGL((rope_kernel<T, V, INTER, true>), grid, dim3(256), 0, st, a, tpg, items, rot_items);
   else hipLaunchKernelGGL((rope_kernel<T, V, INTER, false>), grid, dim3(256), 0, st, a, tpg, items, rot_items);
   return hipGetLastError();

@@ -127,6 +127,24 @@ def test_append(cuda, rolling, dtype, D, rot, interleaved, layout):
         assert torch.equal(order(kcd, layout).cpu(), kc) and torch.equal(order(vcd, layout).cpu(), vc), step
 
 
+def test_more_tokens_than_one_grid_dimension_takes(cuda):
+    """2^27 and some tokens of one pair: over 2^24 work groups of 8 tokens (a launch counts a dimension's threads
+    in 32 bits).  The sine and cosine of an angle, float32 from the 64-bit turns, are off by under 1e-6."""
+    S = (1 << 27) + 11
+    q = torch.ones(1, 1, S, 2, dtype=torch.float32, device=cuda)
+    f = cattn.rope_frequencies(2).to(cuda) * 1e-3
+    say(f"rope S{S} D2")
+    o, _ = cattn.rope_fwd(q, None, f, q_out=q)
+    third = (S + 7) // 8 // 3 * 8  # about where a third of the work groups ends
+    at = torch.cat([torch.arange(64), *(torch.arange(third * i - 64, third * i + 64) for i in (1, 2)), torch.arange(S - 64, S)])
+    got, angle = o[0, 0, at.to(cuda)].cpu().double(), at.double() * float(f[0])
+    ref = torch.stack([angle.cos() - angle.sin(), angle.cos() + angle.sin()], -1)
+    assert (got - ref).abs().max() <= 2e-6
+    n = o.double().square_().sum(-1)
+    assert (n - 2).abs().max() <= 1e-5  # every row was turned once or not at all
+    assert int((o[0, 0, 1:] == 1).all(-1).sum()) <= 9  # ... at all: 9 angles have |sin| < 2e-7, whose row may be (1, 1) again
+
+
 def test_append_past_a_linear_cache_is_dropped(cuda):
     g = gen(9)
     q, k, v = (randn(g, 2, 1, 1, 64).to(cuda) for _ in range(3))
