@@ -437,6 +437,7 @@ cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const vo
   a.lse = const_cast<float*>(lse), a.lens = lens;
   a.ws = workspace, a.far = workspace + 2 * (int64_t)B * Hq * ws_rows(S);
   a.B = B, a.Hq = Hq, a.Hkv = Hkv, a.S = S, a.D = D, a.window = std::min(window, S), a.sinks = std::min(sinks, S);
+  a.grad_scale = a.window == 1 && (a.sinks == 0 || S == 1) ? 0.f : scale;
   a.scale = scale, a.bf16 = dtype == CATTN_BF16;
   (void)hipGetLastError();
   return hip_status(launch_swa_bwd(a, (hipStream_t)stream));

@@ -95,6 +95,9 @@ struct SwaArgs {
   float* far;       // partial dK, dV of the sink keys (swa_far_floats)
   int B, Hq, Hkv, S, D, window, sinks;  // window in [1, S], sinks in [0, S]
   float scale;
+  // backward: of dQ and dK; 0 where every query sees one key (its probability is 1
+  // whatever its score, so that both are 0 exactly, not what two sums differ by)
+  float grad_scale;
   bool bf16;
 };
 struct SwaDecodeArgs {

@@ -521,7 +521,7 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
   if constexpr (SPLIT > 1) wait_vm(0);  // the rings' last copies
   bf16* row = out_row(my_q);
   sum_parts<D, QG, SPLIT>((f32x4*)smem, w, h, lane, acc, [&](int col, const f32x4& v) {
-    if (my_q < len) store4<bf16>(row + col, v[0] * a.scale, v[1] * a.scale, v[2] * a.scale, v[3] * a.scale);
+    if (my_q < len) store4<bf16>(row + col, v[0] * a.grad_scale, v[1] * a.grad_scale, v[2] * a.grad_scale, v[3] * a.grad_scale);
     else if (my_q < a.S) store4<bf16>(row + col, 0.f, 0.f, 0.f, 0.f);
   });
 }
@@ -729,7 +729,7 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
       store4<bf16>(out + col, 0.f, 0.f, 0.f, 0.f);
     }
   };
-  sum_parts<D, KG, SPLIT>((f32x4*)smem, w, h, lane, dkacc, [&](int col, const f32x4& v) { put(krow, 0, a.scale, col, v); });
+  sum_parts<D, KG, SPLIT>((f32x4*)smem, w, h, lane, dkacc, [&](int col, const f32x4& v) { put(krow, 0, a.grad_scale, col, v); });
   sum_parts<D, KG, SPLIT>((f32x4*)smem, w, h, lane, dvacc, [&](int col, const f32x4& v) { put(vrow, 1, 1.f, col, v); });
 }
 
@@ -754,7 +754,7 @@ __global__ __launch_bounds__(256) void swa_far_sum_kernel(SwaArgs a, int far_par
   for (int i = 1; i < n; ++i) v += sums[i * quads + q];
   const Strides& st = which ? a.sdv : a.sdk;
   T* out = (T*)(which ? a.dv : a.dk) + b * st.b + hk * st.h + key * st.s + 4 * q;
-  const float f = which ? 1.f : a.scale;
+  const float f = which ? 1.f : a.grad_scale;
   if constexpr (sizeof(T) == 2) store4<bf16>(out, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
   else *(f32x4*)out = v * f;
 }

@@ -217,7 +217,7 @@ void swa_dq_f32_kernel(SwaArgs a, float c) {
     contract_tile<D, G::KJ>(ktr, dp, acc, [&](int j) { kr[j] = row_chunk(kn, j); });
   }
   sum_four<D>(sm, w, lane, acc, [&](int g, const ColBlocks<D>& v) {
-    if (my_q < len) store_cols<D>(row, g, h, v, a.scale);
+    if (my_q < len) store_cols<D>(row, g, h, v, a.grad_scale);
   });
 }
 
@@ -343,7 +343,7 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
   float* krow = (float*)a.dk + b * a.sdk.b + hk * a.sdk.h + my_k * a.sdk.s;
   float* vrow = (float*)a.dv + b * a.sdv.b + hk * a.sdv.h + my_k * a.sdv.s;
   sum_four<D>(sm, w, lane, dvacc, [&](int g, const ColBlocks<D>& v) { put(vrow, 1, 1.f, g, v); });
-  sum_four<D>(sm, w, lane, dkacc, [&](int g, const ColBlocks<D>& v) { put(krow, 0, a.scale, g, v); });
+  sum_four<D>(sm, w, lane, dkacc, [&](int g, const ColBlocks<D>& v) { put(krow, 0, a.grad_scale, g, v); });
 }
 
 template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {

@@ -54,6 +54,14 @@ def check(cuda, B, Hq, Hkv, S, D, window, sinks, dtype, lens=None, layout="bhsd"
     return o, lse, g
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,window,sinks", [(70, 1, 0), (1, 5, 3)])
+def test_one_visible_key_has_no_gradient(cuda, S, window, sinks, dtype):
+    """Its probability is 1 whatever its score: dq and dk are 0 exactly, dv the sum of the group's do."""
+    o, lse, g = check(cuda, 2, 4, 2, S, 64, window, sinks, dtype)
+    assert not g["dq"].any() and not g["dk"].any() and g["dv"].any()
+
+
 # window and sinks where tiles of 32 begin and end; S of one token, one tile, several
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [64, 128])
