@@ -27,6 +27,38 @@ struct Lanes {
   }
 };
 
+// One head's matrix, rows rs elements apart, S rows; rows past S - 1 are read from
+// row S - 1.  A tile's uniform address and 32-bit lane offsets (rs < 2^23), of few
+// instructions each.  Against a 64-bit row per lane and load (F32Mat), which took 16
+// registers more and the forward at D = 64 its third wave per SIMD, forward /
+// backward, us: B2 H12/4 S777 D64 window 200 24.6 / 77.5 -> 22.0 / 74.0, B4 H16/4
+// S2048 D64 window 512 168 / 598 -> 158 / 522, D128 298 / 1062 -> 305 / 1046; where
+// the grid is then resident at once, and the window the whole sequence, the heaviest
+// tiles meet on a CU: B1 H12 S2048 D64 70 / 262 -> 78 / 233.
+template <int D> struct TileMat {
+  typedef F32Geom<D> G;
+  const float* p;
+  int rs, S;
+  int h, r;  // this lane: half, index within the half
+
+  __device__ __forceinline__ const char* at(int row0) const { return (const char*)(p + (int64_t)row0 * rs); }
+  // this lane's row of the 32 at row0
+  __device__ __forceinline__ const float* row_ptr(int row0) const {
+    return (const float*)(at(row0) + (unsigned)(__mul24(min(r, S - 1 - row0), rs) + 4 * h) * 4u);
+  }
+  // all of its row fragments
+  __device__ __forceinline__ void rows(int row0, typename G::RowFrags& f) const {
+    const float* g = row_ptr(row0);
+#pragma unroll
+    for (int j = 0; j < G::KJ; ++j) f[j] = row_chunk(g, j);
+  }
+  // transposed fragment of step a of the 32 rows at row0
+  __device__ __forceinline__ typename G::vec trans_step(int row0, int a) const {
+    const int row = min(acc_row(a, 0), S - 1 - row0 - 4 * h);  // and 4 h on
+    return *(const typename G::vec*)(at(row0) + (unsigned)(__mul24(row, rs) + (__mul24(4 * h, rs) + G::DT * r)) * 4u);
+  }
+};
+
 template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, 10)))
 void swa_fwd_f32_kernel(SwaArgs a, float c) {
@@ -51,9 +83,9 @@ void swa_fwd_f32_kernel(SwaArgs a, float c) {
   }
   if (qw >= len) return;
   const KeyTiles kt(qw, min(len, qw + 32), a.window, a.sinks);
-  const F32Mat<D, true> Qm{(const float*)a.q + b * a.sq.b + hq * a.sq.h, (int)a.sq.s, len, h, r};
-  const F32Mat<D, true> Km{(const float*)a.k + b * a.sk.b + hk * a.sk.h, (int)a.sk.s, len, h, r};
-  const F32Mat<D, true> Vm{(const float*)a.v + b * a.sv.b + hk * a.sv.h, (int)a.sv.s, len, h, r};
+  const TileMat<D> Qm{(const float*)a.q + b * a.sq.b + hq * a.sq.h, (int)a.sq.s, len, h, r};
+  const TileMat<D> Km{(const float*)a.k + b * a.sk.b + hk * a.sk.h, (int)a.sk.s, len, h, r};
+  const TileMat<D> Vm{(const float*)a.v + b * a.sv.b + hk * a.sv.h, (int)a.sv.s, len, h, r};
 
   typename G::RowFrags kr;
   if (w < kt.n) Km.rows(kt.tile(w) * 32, kr);
@@ -165,11 +197,11 @@ void swa_dq_f32_kernel(SwaArgs a, float c) {
   }
   if (qw >= len) return;
   const KeyTiles kt(qw, min(len, qw + 32), a.window, a.sinks);
-  const F32Mat<D, true> Qm{(const float*)a.q + b * a.sq.b + hq * a.sq.h, (int)a.sq.s, len, h, r};
-  const F32Mat<D, true> Om{(const float*)a.o + b * a.so.b + hq * a.so.h, (int)a.so.s, len, h, r};
-  const F32Mat<D, true> dOm{(const float*)a.dout + b * a.sdo.b + hq * a.sdo.h, (int)a.sdo.s, len, h, r};
-  const F32Mat<D, true> Km{(const float*)a.k + b * a.sk.b + hk * a.sk.h, (int)a.sk.s, len, h, r};
-  const F32Mat<D, true> Vm{(const float*)a.v + b * a.sv.b + hk * a.sv.h, (int)a.sv.s, len, h, r};
+  const TileMat<D> Qm{(const float*)a.q + b * a.sq.b + hq * a.sq.h, (int)a.sq.s, len, h, r};
+  const TileMat<D> Om{(const float*)a.o + b * a.so.b + hq * a.so.h, (int)a.so.s, len, h, r};
+  const TileMat<D> dOm{(const float*)a.dout + b * a.sdo.b + hq * a.sdo.h, (int)a.sdo.s, len, h, r};
+  const TileMat<D> Km{(const float*)a.k + b * a.sk.b + hk * a.sk.h, (int)a.sk.s, len, h, r};
+  const TileMat<D> Vm{(const float*)a.v + b * a.sv.b + hk * a.sv.h, (int)a.sv.s, len, h, r};
 
   typename G::RowFrags kr;
   if (w < kt.n) Km.rows(kt.tile(w) * 32, kr);
@@ -250,7 +282,7 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
   // this wave's positions w, w + 4, ... of the walk: query tile j of head `head`
   int head = n > w ? (x0 + w) / nj : 0, j = n > w ? jlo + (x0 + w) % nj : 0;
   auto matrix = [&](const void* p, const Strides& s, int hd) {
-    return F32Mat<D, true>{(const float*)p + b * s.b + ((int64_t)hk * group + hd) * s.h, (int)s.s, len, h, r};
+    return TileMat<D>{(const float*)p + b * s.b + ((int64_t)hk * group + hd) * s.h, (int)s.s, len, h, r};
   };
   const float* Lb = a.lse + ((int64_t)b * a.Hq + hk * group) * a.S;
   const float* Db = a.ws + ((int64_t)b * a.Hq + hk * group) * 2 * Sp;
@@ -269,8 +301,8 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
   f32x4* vf = kf + G::KJ * 64;
   {
     // keys past the sequence's end: 0
-    const F32Mat<D, true> Km{(const float*)a.k + b * a.sk.b + hk * a.sk.h, (int)a.sk.s, a.S, h, r};
-    const F32Mat<D, true> Vm{(const float*)a.v + b * a.sv.b + hk * a.sv.h, (int)a.sv.s, a.S, h, r};
+    const TileMat<D> Km{(const float*)a.k + b * a.sk.b + hk * a.sk.h, (int)a.sk.s, a.S, h, r};
+    const TileMat<D> Vm{(const float*)a.v + b * a.sv.b + hk * a.sv.h, (int)a.sv.s, a.S, h, r};
 #pragma unroll
     for (int i = 0; i < G::KJ / 4; ++i) {
       const int q = w + 4 * i;
