@@ -22,8 +22,22 @@
 //  * Padded batches: rows from lens[b] on are never read (a tile that reaches
 //    past the end repeats the last row, masked), so they may hold anything;
 //    their O and gradients are 0 and their LSE -inf.
-#include <limits.h>
-
+//
+// Rounded to bf16, by at most 2^-8 of the value: P and dS, since the matrix cores
+// take bf16 operands (the sums over keys average it out), O, from which the
+// backward forms D, and the gradients as they are stored.  Scores, softmax
+// statistics, D, LSE and all sums are float32.  dQ and dK come out 2.5e-3 off in
+// the 2-norm where a float32 computation rounded once is 1.7e-3 off, and 3.8e-3 at
+// window 2, where dP - D cancels.
+//
+// Bound, on full grids, by what a SIMD issues: a forward block at D = 64 is 256
+// cycles of the matrix cores and about 500 of vector instructions, half of them
+// the 16 exponentials; it measures 600 with three waves per SIMD.  Small grids and
+// narrow windows are bound by the first tiles' way from HBM (B8 H12 S1024 D64,
+// forward / backward, us: window 1 12.4 / 31.9, 256 19.5 / 49.9, 1024 24.8 / 69.7; q,
+// k, v and o alone take 10 at 5.15 TB/s).  Measured, B2 H16 S8192 D128, TFLOP/s of 4 D
+// / 10 D operations per visible pair: window 512 608 / 485, 1024 814 / 628, 4096
+// 1009 / 761, no window 1081 / 800 (causal kernels: 1108 / 830).
 #include <algorithm>
 #include <utility>
 
@@ -291,12 +305,7 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
         if (ks + 1 < KS_D) ka[(ks + 1) & 1] = fr.row(t, ks + 1);
         s = MB::run(ka[ks & 1], qf[ks], s);
       }
-      if (wt.masked(x)) {
-        const int key = kt.tile(x) * 32 + 4 * opaque(h);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
-      }
+      if (wt.masked(x)) swa_mask(s, swa_keys(my_q, kt.tile(x) * 32 + 4 * opaque(h), a.window, a.sinks));
       f32x16 pv;
       float psum = block_exp(s, c, m * c, pv);
       if (__builtin_amdgcn_ballot_w64(!(psum <= kSumMax))) {  // rare: move the offset
@@ -505,12 +514,7 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
         s = MB::run(ka[ks & 1], qf[ks], s);
         dx = MB::run(va[ks & 1], dof[ks], dx);  // D - dP^T
       }
-      if (wt.masked(x)) {
-        const int key = kt.tile(x) * 32 + 4 * opaque(h);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
-      }
+      if (wt.masked(x)) swa_mask(s, swa_keys(my_q, kt.tile(x) * 32 + 4 * opaque(h), a.window, a.sinks));
 #pragma unroll
       for (int e = 0; e < 16; ++e) dx[e] = -exp2_hw(fmaf(s[e], c, -lse2)) * dx[e];  // dS^T = P (dP - D)
       const MB::frag db[2] = {MB::pack(dx, 0), MB::pack(dx, 1)};
@@ -679,15 +683,9 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
       }
       // s[e], dx[e]: S - LSE/scale and D - dP of query 32 jw + acc_row(e, h), key my_k
       if (jw <= wdiag || (FAR ? jw < wedge : jw >= wedge) || jw == jrag) {
-        const int qs = jw * 32;
-        const int key = opaque(my_k), qry = qs + 4 * opaque(h);
-        const int low = FAR ? a.window : 0;  // the pair counts where low <= query - key < high
-        const int high = FAR ? (key < a.sinks ? INT_MAX : 0) : key < sinks ? INT_MAX : a.window;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int q = qry + acc_row(e, 0), ahead = q - key;
-          s[e] = swa_masked((ahead >= low) & (ahead < high) & (q < len), s[e]);
-        }
+        const int key = opaque(my_k), qry = jw * 32 + 4 * opaque(h);
+        const bool to_end = key < (FAR ? a.sinks : sinks);  // (a far pair is seen by sinks only)
+        swa_mask(s, swa_queries(FAR ? key + a.window : key, to_end ? len : FAR ? 0 : min(key + a.window, len), qry));
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {

@@ -208,9 +208,7 @@ __global__ __launch_bounds__(256) void swa_decode_bf16_kernel(SwaDecodeArgs a, f
       int count;
       st.slot(t0 + w + 4 * i, count);
       if (count < 32) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[e] = swa_masked(acc_row(e, h) < count, s[e]);
+        swa_mask(s, bits_below(count - 4 * h));
       }
       online_softmax(s, c, run, [&](float alpha) {
 #pragma unroll
@@ -278,9 +276,7 @@ __global__ __launch_bounds__(256) void swa_decode_f32_kernel(SwaDecodeArgs a, fl
     typename G::TransFrags vt;
     f32x16 s = contract_rows<D, 16>(kr, sm, lane, f32x16{}, [&](int e) { vt[e] = Vm.trans_step(0, e); });
     if (count < 32) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        s[e] = swa_masked(acc_row(e, h) < count, s[e]);
+      swa_mask(s, bits_below(count - 4 * h));
     }
     online_softmax(s, c, run, [&](float alpha) {
 #pragma unroll

@@ -36,13 +36,34 @@ __device__ __forceinline__ int swa_head(int i, int n, int group) {
   return n % 8 == 0 ? (i & 7) * (n >> 3) + (i >> 3) : i;
 }
 
-// Masks are selects of conditions joined by & and |.  With && and || the compiler
-// (ROCm 7.2's) made branches of them, and in one kernel lost the assignment of an
-// accumulator's first element in the branch: hidden pairs kept their score.
-__device__ __forceinline__ bool swa_sees(int query, int key, int window, int sinks) {
-  return (key <= query) & ((query - key < window) | (key < sinks));
+// Masks of a score block.  Its 16 elements of a lane are rows base + acc_row(e, 0)
+// of a tile, base = first row + 4 half: bits 0 .. 27 of a word, set where the pair
+// is seen, formed once per lane and tile from the ends of what its column sees; an
+// element then takes two instructions (bit to all ones, bitwise select).  With
+// comparisons per element, six, a masked tile cost a wave 450 cycles: B8 H12 S1024
+// D64 window 32 / 256, forward 16.1 / 20.7 -> 14.9 / 19.6 us; B4 H16 S2048 D128 window
+// 256 46.9 -> 44.7.
+// (Comparisons joined by && and || were wrong besides: the compiler, ROCm 7.2's, made
+// branches of them, and in one kernel lost the assignment of an accumulator's first
+// element in the branch, so that hidden pairs kept their score.)
+__device__ __forceinline__ unsigned bits_below(int n) { return (1u << min(max(n, 0), 31)) - 1; }  // bits 0 .. n - 1 (of 28)
+// Keys from key0 on that `query` sees.
+__device__ __forceinline__ unsigned swa_keys(int query, int key0, int window, int sinks) {
+  const int n = query - key0 + 1;
+  return bits_below(n) & (~bits_below(n - window) | bits_below(sinks - key0));
 }
-__device__ __forceinline__ float swa_masked(bool seen, float score) { return seen ? score : -INFINITY; }
+// Queries lo .. hi - 1, from query0 on.
+__device__ __forceinline__ unsigned swa_queries(int lo, int hi, int query0) {
+  return bits_below(hi - query0) & ~bits_below(lo - query0);
+}
+__device__ __forceinline__ void swa_mask(f32x16& s, unsigned seen) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float score = s[e];  // (a bit cast of the element itself reads element 0)
+    const int keep = __builtin_amdgcn_sbfe(seen, acc_row(e, 0), 1), bits = __builtin_bit_cast(int, score);
+    s[e] = __builtin_bit_cast(float, (keep & bits) | (~keep & (int)0xff800000));  // or -inf
+  }
+}
 
 // The 32-key tiles that queries [q0, q1) see: the sinks' tiles 0 .. sink_tiles-1,
 // then first .. first + n - sink_tiles - 1.

@@ -6,8 +6,6 @@
 // the fixed operand in LDS.  Which tiles are visited and masked, grouped heads,
 // the sinks' far queries and padded batches are as in the bf16 kernels
 // (swa_bf16.hip).
-#include <limits.h>
-
 #include "attn_launch.h"
 #include "f32_stream.h"
 #include "swa_device.h"
@@ -101,12 +99,7 @@ void swa_fwd_f32_kernel(SwaArgs a, float c) {
     const int k0 = kt.tile(x) * 32;
     typename G::TransFrags vt;
     f32x16 s = contract_rows<D, 16>(kr, sm, lane, f32x16{}, [&](int e) { vt[e] = Vm.trans_step(k0, e); });
-    if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
-      const int key = k0 + 4 * opaque(h);
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
-    }
+    if (swa_tile_masked(qw, k0, a.window, a.sinks)) swa_mask(s, swa_keys(my_q, k0 + 4 * opaque(h), a.window, a.sinks));
     float mx = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
@@ -237,12 +230,7 @@ void swa_dq_f32_kernel(SwaArgs a, float c) {
     const float* vp = Vm.row_ptr(k0);
     f32x16 s = contract_rows<D, G::KJ>(kr, qf, lane, f32x16{}, [&](int j) { vr[j] = row_chunk(vp, j); });
     f32x16 dp = contract_rows<D, 16>(vr, dof, lane, f32x16{}, [&](int e) { ktr[e] = Km.trans_step(k0, e); });
-    if (swa_tile_masked(qw, k0, a.window, a.sinks)) {
-      const int key = k0 + 4 * opaque(h);
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        s[e] = swa_masked(swa_sees(my_q, key + acc_row(e, 0), a.window, a.sinks), s[e]);
-    }
+    if (swa_tile_masked(qw, k0, a.window, a.sinks)) swa_mask(s, swa_keys(my_q, k0 + 4 * opaque(h), a.window, a.sinks));
 #pragma unroll
     for (int e = 0; e < 16; ++e) dp[e] = exp2_hw(fmaf(s[e], c, -lse2)) * (dp[e] - Dq);  // dS^T
     const float* kn = Km.row_ptr(kt.tile(x + 4 < kt.n ? x + 4 : x) * 32);
@@ -338,13 +326,8 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
     const bool masked = FAR ? q0 - (kw + 31) < a.window || kw + 32 > a.sinks : q0 < kw + 31 || q0 + 31 - kw >= a.window;
     if (masked || q0 + 32 > len) {
       const int key = opaque(my_k), qry = q0 + 4 * opaque(h);
-      const int low = FAR ? a.window : 0;  // the pair counts where low <= query - key < high
-      const int high = FAR ? (key < a.sinks ? INT_MAX : 0) : key < sinks ? INT_MAX : a.window;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int q = qry + acc_row(e, 0), ahead = q - key;
-        s[e] = swa_masked((ahead >= low) & (ahead < high) & (q < len), s[e]);
-      }
+      const bool to_end = key < (FAR ? a.sinks : sinks);  // (a far pair is seen by sinks only)
+      swa_mask(s, swa_queries(FAR ? key + a.window : key, to_end ? len : FAR ? 0 : min(key + a.window, len), qry));
     }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
