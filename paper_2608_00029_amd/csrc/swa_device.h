@@ -43,9 +43,6 @@ __device__ __forceinline__ int swa_head(int i, int n, int group) {
 // comparisons per element, six, a masked tile cost a wave 450 cycles: B8 H12 S1024
 // D64 window 32 / 256, forward 16.1 / 20.7 -> 14.9 / 19.6 us; B4 H16 S2048 D128 window
 // 256 46.9 -> 44.7.
-// (Comparisons joined by && and || were wrong besides: the compiler, ROCm 7.2's, made
-// branches of them, and in one kernel lost the assignment of an accumulator's first
-// element in the branch, so that hidden pairs kept their score.)
 __device__ __forceinline__ unsigned bits_below(int n) { return (1u << min(max(n, 0), 31)) - 1; }  // bits 0 .. n - 1 (of 28)
 // Keys from key0 on that `query` sees.
 __device__ __forceinline__ unsigned swa_keys(int query, int key0, int window, int sinks) {
