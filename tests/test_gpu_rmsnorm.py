@@ -93,6 +93,37 @@ def test_empty_and_shapes(cuda):
     assert cattn.rmsnorm_fwd(x, gamma)[0].shape == (2, 3, 64) and cattn.rmsnorm_fwd(x, gamma)[2].shape == (6,)
 
 
+@pytest.mark.parametrize("rows,C", [(700, 768), (90, 4096)])
+def test_a_replayed_graph_and_two_streams(cuda, rows, C):
+    x, r, dy = (randn(gen(40 + i), rows, C, dtype="bf16").to(cuda) for i in range(3))
+    gamma = torch.ones(C, device=cuda)
+
+    def run():
+        y, h, rstd = cattn.rmsnorm_fwd(x, gamma, r)
+        q, scale, _, _ = cattn.rmsnorm_fwd_q8(x, gamma, r, group=64)
+        return (y, h, rstd, q.view(torch.uint8), scale) + cattn.rmsnorm_bwd(h, gamma, rstd, dy, r)
+
+    first = run()
+    torch.cuda.synchronize()
+    results = []
+    for s in [torch.cuda.Stream(), torch.cuda.Stream()] * 2:
+        with torch.cuda.stream(s):
+            results.append(run())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for got in results for a, b in zip(first, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = run()
+    for _ in range(3):
+        x.copy_(torch.roll(x, 1, 0))
+        gamma += 0.25
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, want))
+
+
 def test_repeats_bit_for_bit_and_refuses(cuda):
     x, dy = randn(gen(5), 3000, 1600).to(cuda), randn(gen(6), 3000, 1600).to(cuda)
     gamma = torch.ones(1600, device=cuda)

@@ -127,6 +127,36 @@ def test_append(cuda, rolling, dtype, D, rot, interleaved, layout):
         assert torch.equal(order(kcd, layout).cpu(), kc) and torch.equal(order(vcd, layout).cpu(), vc), step
 
 
+def test_empty_sizes_and_a_replayed_graph(cuda):
+    f = cattn.rope_frequencies(64).to(cuda)
+    for shape in ((0, 2, 3, 64), (2, 2, 0, 64)):
+        e = torch.empty(shape, device=cuda)
+        assert cattn.rope_fwd(e, e, f)[1].shape == shape
+        cache = torch.empty(shape[0], 2, 8, 64, device=cuda)
+        lens = torch.zeros(shape[0], dtype=torch.int32, device=cuda)
+        assert cattn.rope_append(e, e, e, cache, cache.clone(), lens, f)[0].shape == shape
+    q, k = (randn(gen(30), 2, h, 70, 64, dtype="bf16").to(cuda) for h in (4, 2))
+    pos = torch.arange(70, dtype=torch.int32, device=cuda)
+
+    def run():
+        turned = cattn.rope_fwd(q, k, f, pos)
+        return turned + cattn.rope_bwd(*turned, f, pos)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = run()
+    for _ in range(3):
+        pos += 1000
+        q.copy_(torch.roll(q, 1, 2))
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, want))
+
+
 def test_more_tokens_than_one_grid_dimension_takes(cuda):
     """2^27 and some tokens of one pair: over 2^24 work groups of 8 tokens (a launch counts a dimension's threads
     in 32 bits).  The sine and cosine of an angle, float32 from the 64-bit turns, are off by under 1e-6."""

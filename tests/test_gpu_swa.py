@@ -164,6 +164,24 @@ def test_strided_views(cuda, dtype):
         cattn.swa_bwd(qc, kb, vb, o2, do, lse2, 0.125, window, sinks, lens, "bshd", dk=kb)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_expanded_inputs_and_empty_sizes(cuda, dtype):
+    """One key/value sequence for the whole batch, one gradient for all heads: views of stride 0."""
+    q, k, v, do = (t.to(cuda) for t in inputs(8, 3, 4, 2, 90, 64, dtype))
+    k, v, do = k[:1].expand(3, -1, -1, -1), v[:1].expand(3, -1, -1, -1), do[:, :1].expand(-1, 4, -1, -1)
+    o, lse = cattn.swa_fwd(q, k, v, 0.125, 20, 2)
+    got = cattn.swa_bwd(q, k, v, o, do, lse, 0.125, 20, 2)
+    k, v, do = (t.contiguous() for t in (k, v, do))
+    want_o, want_lse = cattn.swa_fwd(q, k, v, 0.125, 20, 2)
+    assert torch.equal(o, want_o) and torch.equal(lse, want_lse)
+    assert all(torch.equal(a, b) for a, b in zip(got, cattn.swa_bwd(q, k, v, o, do, lse, 0.125, 20, 2)))
+    for shape in ((0, 4, 5, 64), (2, 4, 0, 64)):
+        e = q.new_empty(shape)
+        o, lse = cattn.swa_fwd(e, e, e, 0.125, 4, 1)
+        g = cattn.swa_bwd(e, e, e, o, e, lse, 0.125, 4, 1)
+        assert o.shape == shape and lse.shape == shape[:3] and all(t.shape == shape for t in g)
+
+
 def test_repeats_and_streams(cuda):
     """The same bits every time, on another stream, and on two streams at once with workspaces of their own."""
     q, k, v, do = (t.to(cuda) for t in inputs(5, 2, 8, 2, 700, 64, "bf16"))

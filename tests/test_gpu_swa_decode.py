@@ -123,6 +123,18 @@ def test_offsets_past_32_bits(cuda):
     assert torch.equal(kc[0, 0, n], kr[0, 0, 0]) and torch.equal(vc[0, 0, n], t[0, 0, 0]) and not kc[0, 0, n + 1:].any()
 
 
+def test_empty_batch_and_an_expanded_cache(cuda):
+    """No sequences; and one cache read by every sequence of a batch (stride 0)."""
+    q, kc, vc = (randn(gen(50 + i), 3, h, 64, dtype="bf16").to(cuda) for i, h in enumerate((4, 2, 2)))
+    kc, vc = (t[:1, :, None].expand(3, 2, 40, 64) + torch.arange(40, device=cuda)[:, None] % 3 for t in (kc, vc))
+    lens = torch.tensor([40, 7, 0], dtype=torch.int32, device=cuda)
+    want = cattn.swa_decode(q, kc, vc, lens, 0.125, 20, 2)
+    got = cattn.swa_decode(q, kc[:1].expand(3, -1, -1, -1), vc[:1].expand(3, -1, -1, -1), lens, 0.125, 20, 2)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    o, lse = cattn.swa_decode(q[:0], kc[:0].contiguous(), vc[:0].contiguous(), lens[:0], 0.125, 20, 2)
+    assert o.shape == (0, 4, 64) and lse.shape == (0, 4)
+
+
 def test_refusals(cuda):
     q, c = torch.zeros(2, 4, 64, device=cuda), torch.zeros(2, 2, 40, 64, device=cuda)
     lens = torch.ones(2, dtype=torch.int32, device=cuda)
