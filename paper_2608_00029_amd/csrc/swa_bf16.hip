@@ -62,45 +62,42 @@ template <int OFF> __device__ __forceinline__ void dma16_at(const void* sbase, u
 #pragma clang diagnostic pop
 
 // HBM -> LDS copies of pairs of 32-row tiles (K and V, or Q and dO) by a work
-// group of W waves.  A wave copies 1 KB pieces: with more waves than a tile has
-// pieces, the first half of them takes one tile and the others the other.  A
-// lane's offsets inside a tile are fixed for the kernel; a tile that reaches past
-// the sequence's end, whose rows past row `last` repeat it, forms its own.
-// (Row strides stay below 2^23: 24-bit products.)  TIGHT, for dK/dV at D = 128,
-// whose registers are all in use: one register per tensor and one for the chunk
-// instead of two per tensor, an addition of three terms per copy.
+// group of W waves, in 1 KB pieces, every wave some of both tiles.  A lane's
+// offsets inside a tile are fixed for the kernel; a tile that reaches past the
+// sequence's end, whose rows past row `last` repeat it, forms its own.  (Row
+// strides stay below 2^23: 24-bit products.)  TIGHT, for dK/dV at D = 128, whose
+// registers are all in use: one register per tensor and one for the chunk instead
+// of two per tensor, an addition of three terms per copy.
 template <int D, int W, bool TIGHT = false> struct SwaCopy {
   static constexpr int TILE = TileGeom<D>::TILE, PIECES = TILE / 1024, CPR = TileGeom<D>::CPR;
-  static constexpr bool BOTH = W <= PIECES;  // every wave copies from both tiles
-  static constexpr int N = BOTH ? PIECES / W : 1, STEP = 64 * W / CPR;
-  static constexpr int PER_PAIR = BOTH ? 2 * N : 1;  // copies of each wave
-  static_assert(BOTH || W == 2 * PIECES, "one piece per wave");
+  static constexpr int N = PIECES / W, STEP = 64 * W / CPR;
+  static constexpr int PER_PAIR = 2 * N;  // copies of each wave
+  static_assert(PIECES % W == 0, "whole pieces");
   static_assert(!TIGHT || (N == 2 && STEP == 16), "the second copy's rows are 16 on: swz(row + 16) = swz(row) ^ 7");
-  unsigned va[TIGHT ? 1 : N], vb[TIGHT ? 1 : N];  // byte offsets of this lane's chunks (vb: BOTH only); TIGHT: its row's
+  unsigned va[TIGHT ? 1 : N], vb[TIGHT ? 1 : N];  // byte offsets of this lane's chunks; TIGHT: of its row
   unsigned chunk;                                 // TIGHT: the chunk's offset in the row
   unsigned lds;  // where this wave's first piece goes
   int w, rsa, rsb;
-  __device__ __forceinline__ bool second() const { return !BOTH && w >= PIECES; }
   __device__ __forceinline__ unsigned offset(int i, int lane, int rs, int last) const {
-    const int p = (BOTH ? w : w % PIECES) * 64 + lane, row = p / CPR + STEP * i;
+    const int p = w * 64 + lane, row = p / CPR + STEP * i;
     return __umul24(min(row, last), 2 * rs) + (((p % CPR) ^ swz(row)) << 4);
   }
   __device__ __forceinline__ void init(const char* smem, int w_, int64_t rsa_, int64_t rsb_) {
     const int lane = threadIdx.x & 63;
     w = w_;
-    lds = lds_addr(smem) + (BOTH ? w : w % PIECES) * 1024 + (second() ? TILE : 0);
+    lds = lds_addr(smem) + w * 1024;
     rsa = (int)rsa_;
     rsb = (int)rsb_;
     if constexpr (TIGHT) {
       chunk = offset(0, lane, 0, 31);
       va[0] = offset(0, lane, rsa, 31) - chunk;
       vb[0] = offset(0, lane, rsb, 31) - chunk;
-      return;
-    }
+    } else {
 #pragma unroll
-    for (int i = 0; i < (TIGHT ? 1 : N); ++i) {
-      va[i] = offset(i, lane, second() ? rsb : rsa, 31);
-      if constexpr (BOTH) vb[i] = offset(i, lane, rsb, 31);
+      for (int i = 0; i < N; ++i) {
+        va[i] = offset(i, lane, rsa, 31);
+        vb[i] = offset(i, lane, rsb, 31);
+      }
     }
   }
   // tile a to byte OFF of the work group's LDS, tile b behind it
@@ -111,25 +108,19 @@ template <int D, int W, bool TIGHT = false> struct SwaCopy {
       const unsigned c1 = chunk ^ 0x70;
       dma16_at<OFF + W * 1024>(a, va[0] + c1 + 32 * rsa, lds);
       dma16_at<OFF + TILE + W * 1024>(b, vb[0] + c1 + 32 * rsb, lds);
-    } else if constexpr (BOTH) {
+    } else {
       unroll<N>([&](auto i) __attribute__((always_inline)) {
         dma16_at<OFF + decltype(i)::value * W * 1024>(a, va[decltype(i)::value], lds);
         dma16_at<OFF + TILE + decltype(i)::value * W * 1024>(b, vb[decltype(i)::value], lds);
       });
-    } else {
-      dma16_at<OFF>(second() ? b : a, va[0], lds);
     }
   }
   template <int OFF> __device__ __forceinline__ void pair_last(const bf16* a, const bf16* b, int last) const {
     const int lane = opaque(threadIdx.x & 63);
-    if constexpr (BOTH) {
-      unroll<N>([&](auto i) __attribute__((always_inline)) {
-        dma16_at<OFF + decltype(i)::value * W * 1024>(a, offset(decltype(i)::value, lane, rsa, last), lds);
-        dma16_at<OFF + TILE + decltype(i)::value * W * 1024>(b, offset(decltype(i)::value, lane, rsb, last), lds);
-      });
-    } else {
-      dma16_at<OFF>(second() ? b : a, offset(0, lane, second() ? rsb : rsa, last), lds);
-    }
+    unroll<N>([&](auto i) __attribute__((always_inline)) {
+      dma16_at<OFF + decltype(i)::value * W * 1024>(a, offset(decltype(i)::value, lane, rsa, last), lds);
+      dma16_at<OFF + TILE + decltype(i)::value * W * 1024>(b, offset(decltype(i)::value, lane, rsb, last), lds);
+    });
   }
 };
 
@@ -229,7 +220,7 @@ template <int D> __device__ __forceinline__ int acc_col(int dt, int g, int h) { 
 // tiles in SPLIT interleaved parts by W = QG * SPLIT waves.
 // ---------------------------------------------------------------------------
 template <int D, int W, int SPLIT, int NB>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 8 ? 2 : SPLIT > 1 ? 1 : D == 128 ? 3 : 4, 10)))
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 128 ? 3 : 4, 10)))
 void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   typedef TileGeom<D> G;
   constexpr int QG = W / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
@@ -416,7 +407,7 @@ __device__ __forceinline__ void sum_parts(f32x4* area, int w, int h, int lane, c
 // contraction starts from D and multiplies by -dO, so it yields D - dP.
 // ---------------------------------------------------------------------------
 template <int D, int W, int SPLIT, int NB>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 8 ? 2 : SPLIT > 1 ? 1 : D == 64 ? 4 : 2, 10)))
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 64 ? 4 : 2, 10)))
 void swa_dq_bf16_kernel(SwaArgs a, float c) {
   typedef TileGeom<D> G;
   constexpr int QG = W / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
