@@ -479,7 +479,7 @@ cattn_status cattn_swa_decode(const void* q, const void* k_cache, const void* v_
                               const int* lens, float* workspace, int B, int Hq, int Hkv, int cap, int D, int window,
                               int sinks, int rolling, float scale, const long long* strides, int layout, int dtype,
                               void* stream);
-size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, int window, int sinks);
+size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, int window, int sinks, int dtype);
 
 /* Bytes of workspace cattn_attn_bwd needs: 2 * B * H * Sp * sizeof(float),
  * Sp = S rounded up to a multiple of 32 (0 for an empty or invalid shape). */

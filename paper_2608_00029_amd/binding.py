@@ -111,7 +111,7 @@ def lib() -> ctypes.CDLL:
         L.cattn_swa_bwd_workspace_bytes.restype = ctypes.c_size_t
         L.cattn_swa_decode.argtypes = [vp] * 7 + [i] * 8 + [f, lp, i, i, vp]
         L.cattn_swa_decode.restype = i
-        L.cattn_swa_decode_workspace_bytes.argtypes = [i] * 7
+        L.cattn_swa_decode_workspace_bytes.argtypes = [i] * 8
         L.cattn_swa_decode_workspace_bytes.restype = ctypes.c_size_t
         L.cattn_status_string.argtypes = [i]
         L.cattn_status_string.restype = ctypes.c_char_p

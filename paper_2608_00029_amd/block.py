@@ -17,8 +17,8 @@ from typing import Optional
 
 import torch
 
-from .binding import (CATTN_OK, CattnError, _check_workspace, _dtype_code, _LAYOUTS, _rows_cols, _stream,
-                      last_error_string, lib)
+from .binding import (CATTN_BF16, CATTN_F32, CATTN_OK, CattnError, _check_workspace, _dtype_code, _LAYOUTS, _rows_cols,
+                      _stream, last_error_string, lib)
 
 _F32, _F64, _I32 = torch.float32, torch.float64, torch.int32
 _SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
@@ -392,8 +392,12 @@ def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens
 
 
 @functools.lru_cache(maxsize=256)
-def swa_decode_workspace_bytes(B: int, Hq: int, Hkv: int, cap: int, D: int, window: int, sinks: int = 0) -> int:
-    return int(lib().cattn_swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, _int(window), _int(sinks)))
+def swa_decode_workspace_bytes(B: int, Hq: int, Hkv: int, cap: int, D: int, window: int, sinks: int = 0,
+                               dtype: Optional[torch.dtype] = None) -> int:
+    """Bytes of swa_decode's workspace; without a dtype what either takes."""
+    sizes = (B, Hq, Hkv, cap, D, _int(window), _int(sinks))
+    codes = {torch.float32: (CATTN_F32,), torch.bfloat16: (CATTN_BF16,)}.get(dtype, (CATTN_F32, CATTN_BF16))
+    return max(int(lib().cattn_swa_decode_workspace_bytes(*sizes, code)) for code in codes)
 
 
 def swa_decode(q, k_cache, v_cache, lens, scale: float, window: int, sinks: int = 0, rolling: bool = False,
@@ -424,7 +428,7 @@ def swa_decode(q, k_cache, v_cache, lens, scale: float, window: int, sinks: int 
         lse = torch.empty((B, Hq), dtype=_F32, device=dev)
     else:
         _plain("lse", lse, (B, Hq), _F32, dev)
-    n = swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, window, sinks) // 4
+    n = swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, window, sinks, dt) // 4
     if workspace is None:
         workspace = lse.new_empty(n) if n else None
     else:

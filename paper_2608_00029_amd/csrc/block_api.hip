@@ -443,10 +443,12 @@ cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const vo
   return hip_status(launch_swa_bwd(a, (hipStream_t)stream));
 }
 
-size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, int window, int sinks) {
+size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, int window, int sinks, int dtype) {
+  if (!valid_dtype(dtype)) return 0;
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || cap <= 0 || D <= 0 || window < 1 || sinks < 0 || Hq % Hkv) return 0;
   return sizeof(float) *
-         (size_t)swa_decode_floats(B, Hq, Hkv, cap, D, std::min(window, cap), std::min(sinks, cap));
+         (size_t)swa_decode_floats(dtype == CATTN_BF16, B, Hq, Hkv, cap, D, std::min(window, cap),
+                                   std::min(sinks, cap));
 }
 
 cattn_status cattn_swa_decode(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
@@ -460,7 +462,7 @@ cattn_status cattn_swa_decode(const void* q, const void* k_cache, const void* v_
   if (rolling && (int64_t)window + sinks > cap)
     return fail(CATTN_ERR_INVALID_ARG, "a rolling cache needs sinks + window <= cap");
   if (empty) return cap == 0 && B && Hq && Hkv ? fail(CATTN_ERR_INVALID_ARG, "cap must be positive") : CATTN_OK;
-  const size_t wsb = cattn_swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, window, sinks);
+  const size_t wsb = cattn_swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, window, sinks, dtype);
   if (!q || !k_cache || !v_cache || !o || !lse || !lens || (wsb && !workspace))
     return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");
   if (!aligned(lse, 4) || !aligned(lens, 4)) return fail(CATTN_ERR_INVALID_ARG, "lse and lens must be 4-byte aligned");

@@ -146,20 +146,39 @@ constexpr int64_t swa_far_floats(int B, int Hq, int Hkv, int S, int D, int windo
   return parts ? (int64_t)B * Hkv * swa_sink_tiles(S, sinks) * (1 + parts) * 2 * 32 * D : 0;
 }
 
-// Decoding: parts that the visible slots of one (sequence, key/value head) are
-// cut into.  Each part is a work group of four waves that stream 32-slot tiles;
-// enough of them to give every CU one, but at least four tiles (one per wave)
-// each.
-constexpr int swa_decode_parts(int B, int Hq, int Hkv, int cap, int window, int sinks) {
-  const int64_t row_blocks = (int64_t)B * Hkv * ((Hq / Hkv + 31) / 32);
+// Decoding: parts that the visible slots of one (sequence, key/value head, 32 query
+// heads) are cut into, each a work group of four waves that stream 32-slot tiles;
+// one of several parts has at least four tiles, one per wave.  Parts cost a second
+// kernel, 4 us, that joins them, so there is one where the slots are few; else as
+// many as give each CU at most one work group (one more is a second round).  In
+// bf16 two or three do not pay: 86 work groups take most of the bandwidth.  In
+// float32, which the matrix cores bound, a second round that is less than full is
+// evened out where it is long.  Time of one token, us, by parts; x: work groups of one part:
+//   bf16  x2 D128    512 slots 1: 7.7, 4: 8.6;  1024 1: 10.5, 8: 8.6;  4096 1: 27.4, 32: 8.8
+//         x16 D64    1024 1: 8.0, 8: 7.9;  2048 1: 11.8, 16: 8.1
+//         x40 D128   1024 1: 11.8, 6: 10.6, 7: 13.7;  4096 1: 29.7, 6: 21.1, 7: 26.0
+//         x80 D128   1024 1: 13.3, 3: 15.5, 4: 19.9;  4096 1: 30.8, 3: 32.4, 4: 36.7
+//         x160 D128  1024 1: 18.0, 2: 25.6;  4096 1: 57.5, 2: 72.6
+//   f32   x2 D128    128 1: 9.6;  256 1: 13.6, 2: 12.8;  x16 D64  256 1: 9.3, 2: 10.2;  512 1: 14.1, 4: 10.2
+//         x48 D64    4096 4: 28.9, 5: 27.1, 6: 35.0;  x160 D128  1024 1: 39.6, 2: 46.6;  4096 1: 147, 2: 166
+//         x320 D128  512 1: 42.4, 3: 44.4;  1024 1: 84.5, 2: 75.2, 3: 73.8;  4096 1: 312, 2: 255, 3: 240
+constexpr int swa_decode_parts(bool bf16, int B, int Hq, int Hkv, int cap, int D, int window, int sinks) {
+  const int64_t blocks = (int64_t)B * Hkv * ((Hq / Hkv + 31) / 32);
   const int64_t seen = (int64_t)window + sinks < cap ? (int64_t)window + sinks : cap;
-  const int64_t most = (seen + 127) / 128, want = (kSwaCus + row_blocks - 1) / row_blocks;
-  const int64_t n = want < most ? want : most;
+  if (seen * D <= (bf16 ? 1 << 16 : 1 << 14)) return 1;
+  int64_t n = kSwaCus / blocks;
+  if (bf16 && n < 4) n = 1;
+  if (!bf16 && blocks > kSwaCus && blocks < 2 * kSwaCus && seen >= 1024) {
+    n = 1;  // the fewest that leave a tenth of the rounds' places empty or less
+    while (n < 4 && (blocks * n + kSwaCus - 1) / kSwaCus * kSwaCus * 10 > 11 * blocks * n) ++n;
+  }
+  const int64_t most = (seen + 127) / 128;
+  n = n < most ? n : most;
   return n < 1 ? 1 : (int)n;
 }
 // Floats of the decode workspace: none for one part, else O [part][B * Hq][D], then offset and sum [part][B * Hq][2].
-constexpr int64_t swa_decode_floats(int B, int Hq, int Hkv, int cap, int D, int window, int sinks) {
-  const int n = swa_decode_parts(B, Hq, Hkv, cap, window, sinks);
+constexpr int64_t swa_decode_floats(bool bf16, int B, int Hq, int Hkv, int cap, int D, int window, int sinks) {
+  const int n = swa_decode_parts(bf16, B, Hq, Hkv, cap, D, window, sinks);
   return n == 1 ? 0 : (int64_t)n * B * Hq * (D + 2);
 }
 

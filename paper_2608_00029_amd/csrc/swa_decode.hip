@@ -344,7 +344,7 @@ __global__ __launch_bounds__(256) void swa_decode_join_kernel(SwaDecodeArgs a, i
 }  // namespace
 
 hipError_t launch_swa_decode(const SwaDecodeArgs& a, hipStream_t st) {
-  const int parts = swa_decode_parts(a.B, a.Hq, a.Hkv, a.cap, a.window, a.sinks);
+  const int parts = swa_decode_parts(a.bf16, a.B, a.Hq, a.Hkv, a.cap, a.D, a.window, a.sinks);
   const int blocks = (a.Hq / a.Hkv + 31) / 32;
   const dim3 grid((unsigned)(a.B * a.Hkv * blocks), (unsigned)parts);
   const float c = a.scale * kLog2e;

@@ -156,8 +156,13 @@ def test_workspace_sizes(lib):
     assert cattn.swa_bwd_workspace_bytes(2, 4, 2, 600, 64, 8, 2 ** 40) > rows  # clamped to the sequence
     assert cattn.swa_bwd_workspace_bytes(2, 3, 2, 40, 64, 8, 2) == 0
     assert cattn.swa_decode_workspace_bytes(300, 8, 8, 4096, 64, 4000) == 0  # work groups enough without parts
-    one = cattn.swa_decode_workspace_bytes(1, 8, 2, 4096, 64, 4000)
-    assert one > 0 and one % (8 * 66 * 4) == 0
+    for dtype in (torch.float32, torch.bfloat16):
+        one = cattn.swa_decode_workspace_bytes(1, 8, 2, 4096, 64, 4000, 0, dtype)
+        assert one > 0 and one % (8 * 66 * 4) == 0
+        assert cattn.swa_decode_workspace_bytes(1, 8, 2, 4096, 64, 200, 50, dtype) == 0  # few slots
+    assert cattn.swa_decode_workspace_bytes(40, 8, 2, 4096, 64, 4000, 0, torch.bfloat16) == 0
+    few, either = (cattn.swa_decode_workspace_bytes(40, 8, 2, 4096, 64, 4000, 0, t) for t in (torch.float32, None))
+    assert few == either == 3 * 40 * 8 * 66 * 4
 
 
 @pytest.mark.parametrize("kw", [dict(), dict(scaling="linear", factor=3.0), dict(scaling="ntk", factor=8.0, base=5e5),

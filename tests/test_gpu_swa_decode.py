@@ -35,7 +35,7 @@ def check(cuda, lens, Hq, Hkv, cap, D, window, sinks, rolling, dtype, layout="bh
         want.append(orc.swa_decode(to64(q[b]), to64(k), to64(v), scale, window, sinks) if n else
                     (np.zeros((Hq, D)), np.full(Hq, -np.inf), np.zeros((Hq, D))))
     kd, vd = (order(t, layout).contiguous().to(cuda) for t in (kc, vc))
-    n = cattn.swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, window, sinks) // 4
+    n = cattn.swa_decode_workspace_bytes(B, Hq, Hkv, cap, D, window, sinks, TYPES[dtype]) // 4
     ws = torch.full((n + 64,), float("nan"), device=cuda)
     o = torch.full((B, Hq, D), float("nan"), dtype=TYPES[dtype], device=cuda)
     lse = torch.full((B, Hq), float("nan"), device=cuda)
@@ -78,6 +78,8 @@ def test_parts(cuda, dtype):
     check(cuda, [3000], 8, 2, 3000, 64, 2500, 3, False, dtype)
     check(cuda, [3000, 200], 8, 1, 4000, 128, 5000, 0, False, dtype)
     check(cuda, [70 + i for i in range(64)], 8, 4, 160, 64, 60, 2, False, dtype)
+    check(cuda, [930 + i for i in range(100)], 6, 3, 1030, 64, 1024, 0, False, dtype)  # over a work group per CU
+    check(cuda, [700, 650, 1], 8, 8, 700, 128, 600, 1, True, dtype)
 
 
 def test_strides_and_lens_past_a_linear_cache(cuda):
