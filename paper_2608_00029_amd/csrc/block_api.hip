@@ -413,6 +413,8 @@ cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const vo
   cattn_status st = swa_sizes(B, Hq, Hkv, S, D, window, sinks, scale, layout, dtype, &empty);
   if (st != CATTN_OK || empty) return st;
   if ((int64_t)B * Hq * ((S + 31) / 32) >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
+  if ((int64_t)B * Hkv * ((S + 31) / 32 + swa_sink_tiles(S, sinks)) >= kMaxGroups)
+    return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
   if ((int64_t)B * Hkv * std::min(sinks, S) >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "too many sinks");
   if (!q || !k || !v || !o || !dout || !lse || !dq || !dk || !dv || !workspace)
     return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");

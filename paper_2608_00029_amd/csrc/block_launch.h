@@ -117,12 +117,12 @@ constexpr int64_t kSwaCus = 256;  // compute units of the one GPU these kernels 
 // dK and dV of the sink keys.  Their queries outside the window reach to the end
 // of the sequence, however long, while every other key has window queries.
 // Where those far queries of all heads of a group are many, the window's work
-// groups leave them out, and a grid of their own takes them: the far (query head,
-// 32-query tile) pairs of a 32-key tile of sinks cut into parts, so that the
-// parts of all heads give the GPU one work group per CU (what its LDS holds at D
-// = 128), but a part has at least a tile for each of its waves.  Each part leaves
-// float32 partial sums.  Backward, 4 sinks, us, with a grid of their own /
-// without, by far queries times heads of the group:
+// groups leave them out, and others take them: the far (query head, 32-query tile)
+// pairs of a 32-key tile of sinks cut into parts, so that the parts of all heads
+// give the GPU one work group per CU (what its LDS holds at D = 128), but a part has
+// at least a tile for each of its waves.  Each part leaves float32 partial sums.
+// Backward, 4 sinks, us, with a grid of their own / without, by far queries times
+// heads of the group:
 //   bf16  256: B1 H4 S1024 D64 35.6 / 27.0;  384: B4 H8 S512 D128 39.6 / 34.5;
 //         768: B1 H4 S1024 D64 28.1 / 25.6, B4 H8 S1024 D128 60.4 / 74.8;
 //         1536: B1 H16/4 S512 D64 30.6 / 37.3;  14336: B1 H16/4 S4096 D128 119 / 475
@@ -132,17 +132,33 @@ constexpr bool swa_has_far(bool bf16, int Hq, int Hkv, int S, int window, int si
   return sinks > 0 && (int64_t)(Hq / Hkv) * (S - window) > (bf16 ? 512 : 400);
 }
 constexpr int swa_sink_tiles(int S, int sinks) { return ((sinks < S ? sinks : S) + 31) / 32; }
-constexpr int swa_far_parts(bool bf16, int B, int Hq, int Hkv, int S, int window, int sinks) {
+// shared: far and window work groups in one grid (kernels that take both), where
+// neither waits for the other; the far ones then need be no shorter than the
+// window's.  Not where a last round would be left for a few of them.  Backward,
+// 4 sinks, us, two grids / shared: bf16 B1 H4 S1024 D64 window 32 20.8 / 15.6, B1
+// H16/4 S1024 D128 window 128 41.5 / 33.5, B2 H12/4 S777 D64 window 200 30.2 / 25.0,
+// but (33 sinks: 312 work groups) B1 H8/2 S4096 D128 window 256 62 / 69; f32 B2 H12/4
+// S777 D64 70 / 61, B4 H16/4 S2048 D128 window 512 1038 / 1006, but (280) B1 H16/4
+// S2000 D64 window 256 104 / 112.
+constexpr int swa_far_parts(bool bf16, bool shared, int B, int Hq, int Hkv, int S, int window, int sinks) {
   if (!swa_has_far(bf16, Hq, Hkv, S, window, sinks)) return 0;
   const int64_t tiles = (int64_t)(Hq / Hkv) * ((S - window + 31) / 32 + 1);
   const int64_t want = kSwaCus / ((int64_t)B * Hkv * swa_sink_tiles(S, sinks)), most = (tiles + 3) / 4;
-  const int64_t n = want < most ? want : most;
+  int64_t n = want < most ? want : most;
+  const int64_t even = (S - window) / (window + 32) + 1;
+  if (shared && n > even) n = even;
   return n < 1 ? 1 : (int)n;
 }
+constexpr bool swa_far_shares(bool bf16, int B, int Hq, int Hkv, int S, int D, int window, int sinks) {
+  const int64_t heads = (int64_t)B * Hkv, walks = heads * ((S + 31) / 32);
+  const int64_t all = walks + heads * swa_sink_tiles(S, sinks) * swa_far_parts(bf16, true, B, Hq, Hkv, S, window, sinks);
+  if (bf16) return all <= (D == 64 ? 2 : 1) * kSwaCus;  // (work groups that fit a CU)
+  return all <= kSwaCus || walks >= 2 * kSwaCus;        // (a second one on a CU takes as long again)
+}
 // Floats of the far area: [B * Hkv][sink tile][1 + parts][dK, dV][32][D]; slot 0
-// is the window's own sum.  (Of either type: what float32 needs.)
+// is the window's own sum.  (What the type and grid that take most of it need.)
 constexpr int64_t swa_far_floats(int B, int Hq, int Hkv, int S, int D, int window, int sinks) {
-  const int parts = swa_far_parts(false, B, Hq, Hkv, S, window, sinks);
+  const int parts = swa_far_parts(false, false, B, Hq, Hkv, S, window, sinks);
   return parts ? (int64_t)B * Hkv * swa_sink_tiles(S, sinks) * (1 + parts) * 2 * 32 * D : 0;
 }
 
@@ -188,6 +204,6 @@ hipError_t launch_swa_decode(const SwaDecodeArgs& a, hipStream_t st);
 hipError_t launch_swa_fwd_f32(const SwaArgs& a, hipStream_t st);
 hipError_t launch_swa_bwd_f32(const SwaArgs& a, hipStream_t st);
 // dK, dV of the sink keys from their partial sums (after the kernels that leave them)
-hipError_t launch_swa_far_sum(const SwaArgs& a, hipStream_t st);
+hipError_t launch_swa_far_sum(const SwaArgs& a, int far_parts, hipStream_t st);
 
 }  // namespace cattn

@@ -16,9 +16,9 @@
 //    work group walks the query tiles of all heads of its group, which sums
 //    the group's gradients in float32 in a fixed order.
 //  * Sinks in dK/dV: a sink's queries reach to the end of the sequence.  The
-//    window's work groups leave out the pairs that only the sinks see, a
-//    second grid takes those in parts (swa_far_parts), and a third sums the
-//    partial results in order: no work group runs longer than the others.
+//    window's work groups leave out the pairs that only the sinks see, others
+//    take those in parts (swa_far_parts), and another kernel sums the partial
+//    results in order: no work group runs longer than the others.
 //  * Padded batches: rows from lens[b] on are never read (a tile that reaches
 //    past the end repeats the last row, masked), so they may hold anything;
 //    their O and gradients are 0 and their LSE -inf.
@@ -524,13 +524,15 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
 // ---------------------------------------------------------------------------
 // Backward, kernel 2: dK, dV.  A work group owns 32 * KG keys of one key/value
 // head and walks, for each query head of the group, the query tiles that see
-// them from the last down, in SPLIT interleaved parts by W = KG * SPLIT waves.  FAR: the pairs that
-// only the sinks see, 32 sink keys and one part of the walk a work group, into
-// the far area; otherwise the pairs of the window.
+// them from the last down, in SPLIT interleaved parts by W = KG * SPLIT waves.  A far
+// work group takes the pairs that only the sinks see, 32 sink keys and one part of
+// the walk, into the far area, the others the pairs of the window.  Where both fit
+// one form they may share a grid (swa_far_shares), the first n_far work groups far.
 // ---------------------------------------------------------------------------
-template <int D, int W, int SPLIT, int NB, bool FAR>
+enum class Pairs { kWindow, kFar, kBoth };
+template <int D, int W, int SPLIT, int NB, Pairs PAIRS>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 8 ? 2 : SPLIT > 1 ? 1 : D == 64 ? 3 : 2, 10)))
-void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
+void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts, int n_far) {
   typedef TileGeom<D> G;
   constexpr int KG = W / SPLIT, BKV = 32 * KG, KS_D = D / 16, DT = D / 32;
   constexpr int TILE = G::TILE, SETB = 2 * TILE, AUX = 2 * 32 * 4, AUX0 = SPLIT * NB * SETB;
@@ -540,26 +542,28 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   __shared__ __attribute__((aligned(16))) char smem[SPLIT * NB * (SETB + AUX)];
   static_assert(SPLIT == 1 || W * 64 * DT * 16 * 4 <= SPLIT * NB * SETB, "merge area");
   static_assert(NB * SETB <= 65536, "tile reads reach every slot by immediate offset");
-  static_assert(!FAR || KG == 1, "a tile of sinks is one key group");
+  static_assert(PAIRS == Pairs::kWindow || KG == 1, "a tile of sinks is one key group");
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = w % KG, part = w / KG;
   const int BH = a.B * a.Hkv, group = a.Hq / a.Hkv;
-  const int bkv = uniform(blockIdx.x % BH), rest = uniform(blockIdx.x / BH);
-  const int chunk = FAR ? uniform(rest % far_parts) : 0, kt = FAR ? uniform(rest / far_parts) : rest;
+  const bool is_far = PAIRS == Pairs::kFar || (PAIRS == Pairs::kBoth && (int)blockIdx.x < n_far);
+  const int at = PAIRS == Pairs::kBoth && !is_far ? blockIdx.x - n_far : blockIdx.x;
+  const int bkv = uniform(at % BH), rest = uniform(at / BH);
+  const int chunk = is_far ? uniform(rest % far_parts) : 0, kt = is_far ? uniform(rest / far_parts) : rest;
   const int b = uniform(bkv / a.Hkv), hk = bkv - b * a.Hkv;
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int k0 = kt * BKV, kw = k0 + 32 * kg, my_k = kw + r;
-  const bool far = FAR || swa_has_far(true, a.Hq, a.Hkv, a.S, a.window, a.sinks);  // sink keys' sums go to the far area
+  const bool far = is_far || swa_has_far(true, a.Hq, a.Hkv, a.S, a.window, a.sinks);  // sink keys' sums go to the far area
   const int sinks = far ? 0 : a.sinks;  // the sinks whose far queries this kernel walks itself
 
   // query tiles jlo .. jhi of every head of the group see a key of this work group
-  const int jlo = FAR ? (k0 + a.window) / 32 : k0 / 32;
-  const int jhi = FAR || k0 < sinks ? (len - 1) / 32 : (min(len, min(k0 + BKV, len) + a.window - 1) - 1) / 32;
-  const int nj = (FAR ? k0 + a.window < len : k0 < len) ? jhi - jlo + 1 : 0;
+  const int jlo = is_far ? (k0 + a.window) / 32 : k0 / 32;
+  const int jhi = is_far || k0 < sinks ? (len - 1) / 32 : (min(len, min(k0 + BKV, len) + a.window - 1) - 1) / 32;
+  const int nj = (is_far ? k0 + a.window < len : k0 < len) ? jhi - jlo + 1 : 0;
   int n = group * nj, x0 = 0;
-  if constexpr (FAR) {
+  if (is_far) {
     const int per = (n + far_parts - 1) / far_parts;
     x0 = chunk * per;
     n = max(0, min(per, n - x0));
@@ -608,11 +612,11 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
     while (at < jlo) at += nj;
   };
   // this wave's tiles: [wlo, whi] hold pairs that count, those up to wdiag and
-  // from wedge on hidden ones too (FAR: those below wedge, or all)
-  const int wlo = FAR ? (max(kw + a.window - 31, 0) + 31) / 32 : kw / 32;
-  const int whi = FAR || kw < sinks ? jhi : kw < len ? (kw + 31 + a.window - 1) / 32 : -1;
-  const int wdiag = FAR ? (kw + 32 > a.sinks ? jhi : -1) : kw / 32;
-  const int wedge = FAR ? (kw + 31 + a.window + 31) / 32 : (max(kw + a.window - 31, 0) + 31) / 32;
+  // from wedge on hidden ones too (is_far: those below wedge, or all)
+  const int wlo = is_far ? (max(kw + a.window - 31, 0) + 31) / 32 : kw / 32;
+  const int whi = is_far || kw < sinks ? jhi : kw < len ? (kw + 31 + a.window - 1) / 32 : -1;
+  const int wdiag = is_far ? (kw + 32 > a.sinks ? jhi : -1) : kw / 32;
+  const int wedge = is_far ? (kw + 31 + a.window + 31) / 32 : (max(kw + a.window - 31, 0) + 31) / 32;
   constexpr int GROUP = ring_group(1, NB, 0, 2);
   ring_prologue<NB, GROUP>(L, dma);
   if (n) advance(jc, part);
@@ -673,10 +677,10 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
         dx = MB::run(da[ks & 1], vf[ks], dx);  // D - dP
       }
       // s[e], dx[e]: S - LSE/scale and D - dP of query 32 jw + acc_row(e, h), key my_k
-      if (jw <= wdiag || (FAR ? jw < wedge : jw >= wedge) || jw == jrag) {
+      if (jw <= wdiag || (is_far ? jw < wedge : jw >= wedge) || jw == jrag) {
         const int key = opaque(my_k), qry = jw * 32 + 4 * opaque(h);
-        const bool to_end = key < (FAR ? a.sinks : sinks);  // (a far pair is seen by sinks only)
-        swa_mask(s, swa_queries(FAR ? key + a.window : key, to_end ? len : FAR ? 0 : min(key + a.window, len), qry));
+        const bool to_end = key < (is_far ? a.sinks : sinks);  // (a far pair is seen by sinks only)
+        swa_mask(s, swa_queries(is_far ? key + a.window : key, to_end ? len : is_far ? 0 : min(key + a.window, len), qry));
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -710,8 +714,8 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts) {
   bf16* krow = (bf16*)a.dk + b * a.sdk.b + hk * a.sdk.h + key * a.sdk.s;
   bf16* vrow = (bf16*)a.dv + b * a.sdv.b + hk * a.sdv.h + key * a.sdv.s;
   auto put = [&](bf16* out, int which, float f, int col, const f32x4& v) {
-    if (FAR || (far && my_k < a.sinks && my_k < len)) {
-      if (!FAR || my_k < a.sinks) *(f32x4*)(swa_far_slot(a, bkv, my_k, FAR ? 1 + chunk : 0, far_parts) + which * 32 * dim + col) = v;
+    if (is_far || (far && my_k < a.sinks && my_k < len)) {
+      if (!is_far || my_k < a.sinks) *(f32x4*)(swa_far_slot(a, bkv, my_k, is_far ? 1 + chunk : 0, far_parts) + which * 32 * dim + col) = v;
     } else if (my_k < len) {
       store4<bf16>(out + col, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
     } else if (my_k < a.S) {
@@ -800,8 +804,8 @@ template <int D, int W, int SPLIT, int NB> hipError_t dq_s(const SwaArgs& a, flo
   return hipGetLastError();
 }
 template <int D, int W, int SPLIT, int NB> hipError_t dkdv_s(const SwaArgs& a, float c, int far, hipStream_t st) {
-  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, W, SPLIT, NB, false>), rows_grid<32 * W / SPLIT>(a, a.Hkv), dim3(64 * W), 0,
-                     st, a, c, far);
+  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, W, SPLIT, NB, Pairs::kWindow>), rows_grid<32 * W / SPLIT>(a, a.Hkv),
+                     dim3(64 * W), 0, st, a, c, far, 0);
   return hipGetLastError();
 }
 
@@ -815,7 +819,6 @@ template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
 }
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
-  const int far = swa_far_parts(true, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
   hipError_t e;
   switch (form_of(Pass::kDq, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
     case kFour: e = dq_s<D, 4, 4, 2>(a, c, st); break;
@@ -823,8 +826,20 @@ template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
     default: e = dq_s<D, 4, 1, 4>(a, c, st);
   }
   if (e != hipSuccess) return e;
-  switch (form_of(Pass::kDkdv, D, (int64_t)a.B * a.Hkv, a.S, run_of(a) * (a.Hq / a.Hkv))) {
-    case kFour: e = dkdv_s<D, 4, 4, 2>(a, c, far, st); break;
+  const Form form = form_of(Pass::kDkdv, D, (int64_t)a.B * a.Hkv, a.S, run_of(a) * (a.Hq / a.Hkv));
+  const bool shared = form == kFour && swa_far_shares(true, a.B, a.Hq, a.Hkv, a.S, a.D, a.window, a.sinks);
+  const int far = swa_far_parts(true, shared, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const int n_far = a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks) * far;
+  switch (form) {
+    case kFour:
+      if (far && shared) {
+        hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 4, 2, Pairs::kBoth>), dim3(n_far + rows_grid<32>(a, a.Hkv).x),
+                           dim3(256), 0, st, a, c, far, n_far);
+        e = hipGetLastError();
+        return e != hipSuccess ? e : launch_swa_far_sum(a, far, st);
+      }
+      e = dkdv_s<D, 4, 4, 2>(a, c, far, st);
+      break;
     case kTwo: e = dkdv_s<D, 4, 2, D == 64 ? 4 : 2>(a, c, far, st); break;
     case kEight:
       if constexpr (D == 128) {
@@ -834,16 +849,14 @@ template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
     default: e = dkdv_s<D, 4, 1, 4>(a, c, far, st);
   }
   if (e != hipSuccess || !far) return e;
-  const unsigned grid = (unsigned)((int64_t)a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks) * far);
-  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 4, 2, true>), dim3(grid), dim3(256), 0, st, a, c, far);
+  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 4, 2, Pairs::kFar>), dim3(n_far), dim3(256), 0, st, a, c, far, n_far);
   e = hipGetLastError();
-  return e != hipSuccess ? e : launch_swa_far_sum(a, st);
+  return e != hipSuccess ? e : launch_swa_far_sum(a, far, st);
 }
 
 }  // namespace
 
-hipError_t launch_swa_far_sum(const SwaArgs& a, hipStream_t st) {
-  const int far = swa_far_parts(a.bf16, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+hipError_t launch_swa_far_sum(const SwaArgs& a, int far, hipStream_t st) {
   const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * (a.sinks < a.S ? a.sinks : a.S)), 2);
   if (a.bf16) hipLaunchKernelGGL((swa_far_sum_kernel<bf16>), grid, dim3(256), 0, st, a, far);
   else hipLaunchKernelGGL((swa_far_sum_kernel<float>), grid, dim3(256), 0, st, a, far);

@@ -241,28 +241,30 @@ void swa_dq_f32_kernel(SwaArgs a, float c) {
   });
 }
 
-template <int D, bool FAR>
+// The first n_far work groups take the sinks' far queries.
+template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, 10)))
-void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
+void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts, int n_far) {
   typedef F32Geom<D> G;
   __shared__ f32x4 sm[f32_lds_units<D, 1, 2>()];
   __shared__ __attribute__((aligned(16))) float aux[4][2][32];  // each wave's tile: LSE, D
   const Lanes l_;
   const int lane = l_.lane, h = l_.h, r = l_.r, w = l_.w;
   const int BH = a.B * a.Hkv, group = a.Hq / a.Hkv;
-  const int bkv = blockIdx.x % BH, rest = blockIdx.x / BH;
-  const int chunk = FAR ? rest % far_parts : 0, kt = FAR ? rest / far_parts : rest;
+  const bool is_far = (int)blockIdx.x < n_far;
+  const int at = is_far ? blockIdx.x : blockIdx.x - n_far, bkv = at % BH, rest = at / BH;
+  const int chunk = is_far ? rest % far_parts : 0, kt = is_far ? rest / far_parts : rest;
   const int b = bkv / a.Hkv, hk = bkv - b * a.Hkv;
   const int len = swa_len(a.lens, b, a.S), Sp = ws_rows(a.S);
   const int kw = kt * 32, my_k = kw + r;
-  const bool far = FAR || swa_has_far(false, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const bool far = is_far || swa_has_far(false, a.Hq, a.Hkv, a.S, a.window, a.sinks);
   const int sinks = far ? 0 : a.sinks;  // the sinks whose far queries this kernel walks itself
 
-  const int jlo = FAR ? (kw + a.window) / 32 : kt;
-  const int jhi = FAR || kw < sinks ? (len - 1) / 32 : (min(len, min(kw + 32, len) + a.window - 1) - 1) / 32;
-  const int nj = (FAR ? kw + a.window < len : kw < len) ? jhi - jlo + 1 : 0;
+  const int jlo = is_far ? (kw + a.window) / 32 : kt;
+  const int jhi = is_far || kw < sinks ? (len - 1) / 32 : (min(len, min(kw + 32, len) + a.window - 1) - 1) / 32;
+  const int nj = (is_far ? kw + a.window < len : kw < len) ? jhi - jlo + 1 : 0;
   int n = group * nj, x0 = 0;
-  if constexpr (FAR) {
+  if (is_far) {
     const int per = (n + far_parts - 1) / far_parts;
     x0 = chunk * per;
     n = max(0, min(per, n - x0));
@@ -323,11 +325,11 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
     aux[w][1][r] = d_row;
     f32x16 s = contract_rows<D, G::KJ>(qr, kf, lane, f32x16{}, [&](int i) { dor[i] = row_chunk(dop, i); });
     f32x16 dp = contract_rows<D, 16>(dor, vf, lane, f32x16{}, [&](int e) { dot[e] = dOm.trans_step(q0, e); });
-    const bool masked = FAR ? q0 - (kw + 31) < a.window || kw + 32 > a.sinks : q0 < kw + 31 || q0 + 31 - kw >= a.window;
+    const bool masked = is_far ? q0 - (kw + 31) < a.window || kw + 32 > a.sinks : q0 < kw + 31 || q0 + 31 - kw >= a.window;
     if (masked || q0 + 32 > len) {
       const int key = opaque(my_k), qry = q0 + 4 * opaque(h);
-      const bool to_end = key < (FAR ? a.sinks : sinks);  // (a far pair is seen by sinks only)
-      swa_mask(s, swa_queries(FAR ? key + a.window : key, to_end ? len : FAR ? 0 : min(key + a.window, len), qry));
+      const bool to_end = key < (is_far ? a.sinks : sinks);  // (a far pair is seen by sinks only)
+      swa_mask(s, swa_queries(is_far ? key + a.window : key, to_end ? len : is_far ? 0 : min(key + a.window, len), qry));
     }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -347,9 +349,9 @@ void swa_dkdv_f32_kernel(SwaArgs a, float c, int far_parts) {
   }
 
   auto put = [&](float* out, int which, float f, int g, const ColBlocks<D>& v) {
-    if (FAR || (far && my_k < a.sinks && my_k < len)) {
-      if (!FAR || my_k < a.sinks)
-        store_cols<D>(swa_far_slot(a, bkv, my_k, FAR ? 1 + chunk : 0, far_parts) + which * 32 * D, g, h, v, 1.f);
+    if (is_far || (far && my_k < a.sinks && my_k < len)) {
+      if (!is_far || my_k < a.sinks)
+        store_cols<D>(swa_far_slot(a, bkv, my_k, is_far ? 1 + chunk : 0, far_parts) + which * 32 * D, g, h, v, 1.f);
     } else if (my_k < a.S) {
       if (my_k < len) store_cols<D>(out, g, h, v, f);
       else store_cols<D>(out, g, h, ColBlocks<D>{}, 0.f);
@@ -370,18 +372,22 @@ template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
   const int64_t tiles = (a.S + 31) / 32;
-  const int far = swa_far_parts(false, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const bool shared = swa_far_shares(false, a.B, a.Hq, a.Hkv, a.S, a.D, a.window, a.sinks);
+  const int far = swa_far_parts(false, shared, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
+  const int n_far = a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks) * far;
   hipLaunchKernelGGL((swa_dq_f32_kernel<D>), dim3((unsigned)(a.B * a.Hq * tiles)), dim3(256), 0, st, a, c);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((swa_dkdv_f32_kernel<D, false>), dim3((unsigned)(a.B * a.Hkv * tiles)), dim3(256), 0, st, a, c,
-                     far);
+  const unsigned walks = (unsigned)(a.B * a.Hkv * tiles);
+  if (far && !shared) {
+    hipLaunchKernelGGL((swa_dkdv_f32_kernel<D>), dim3((unsigned)n_far), dim3(256), 0, st, a, c, far, n_far);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int first = shared ? n_far : 0;
+  hipLaunchKernelGGL((swa_dkdv_f32_kernel<D>), dim3(first + walks), dim3(256), 0, st, a, c, far, first);
   e = hipGetLastError();
-  if (e != hipSuccess || !far) return e;
-  const unsigned grid = (unsigned)((int64_t)a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks) * far);
-  hipLaunchKernelGGL((swa_dkdv_f32_kernel<D, true>), dim3(grid), dim3(256), 0, st, a, c, far);
-  e = hipGetLastError();
-  return e != hipSuccess ? e : launch_swa_far_sum(a, st);
+  return e != hipSuccess || !far ? e : launch_swa_far_sum(a, far, st);
 }
 
 }  // namespace

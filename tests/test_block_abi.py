@@ -103,6 +103,7 @@ def decode(q=P[0], kc=P[1], vc=P[2], o=P[3], lse=P[4], lens=P[5], ws=P[6], B=2, 
     (swa_bwd, dict(dq=P[0]), BAD), (swa_bwd, dict(dk=P[9]), BAD), (swa_bwd, dict(ws=0), BAD), (swa_bwd, dict(ws=P[9] + 16), BAD),
     (swa_bwd, dict(ws=P[10] + 4), BAD), (swa_bwd, dict(do=0), BAD), (swa_bwd, dict(lse=P[7]), BAD), (swa_bwd, dict(D=32), NO),
     (swa_bwd, dict(B=64, Hq=8, Hkv=8, S=1 << 23, sinks=1 << 23), NO), (swa_bwd, dict(B=4, Hq=8, Hkv=8, S=1 << 19, sinks=1 << 19), NO),
+    (swa_bwd, dict(B=1 << 20, Hq=12, Hkv=12, S=2, window=1, sinks=1), NO),
     (swa, dict(B=64, Hq=8, Hkv=8, S=1 << 20), NO), (decode, dict(B=1 << 20, Hq=16, Hkv=1), NO),
     (decode, dict(cap=9), BAD), (decode, dict(ws=0, window=4000, sinks=0), BAD), (decode, dict(lens=0), BAD), (decode, dict(o=P[0]), BAD),
     (decode, dict(cap=0, rolling=0), BAD), (decode, dict(Hq=5), BAD), (decode, dict(ws=P[3], window=4000), BAD),

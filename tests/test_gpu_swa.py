@@ -113,6 +113,13 @@ def test_far_queries_of_the_sinks(cuda, Hq, Hkv, S, window, sinks, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,B", [(64, 8), (128, 8), (128, 16), (64, 20)])
+def test_far_queries_beside_or_within_the_windows_grid(cuda, D, B, dtype):
+    """320 work groups, 256 of them the window's (one round of the GPU's CUs at D = 128), and whole rounds of them."""
+    check(cuda, B, 4, 2, 500, D, 100, 3, dtype, [500 - 31 * (i % 3) for i in range(B)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ends_of_the_softmax(cuda, dtype):
     """Uniform rows, and rows near one-hot whose offset moves."""
     check(cuda, 1, 2, 2, 140, 64, 50, 2, dtype, scale=1e-20)
