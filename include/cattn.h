@@ -440,9 +440,10 @@ cattn_status cattn_rope_append(const void* q, const void* k, const void* v, void
  *             -infinity.  (A value of a token itself that is not finite may reach
  *             rows that do not see it but share its 32-row tile.)
  *   workspace: at least cattn_swa_bwd_workspace_bytes(...) bytes, 16-byte aligned
- * Supported: D in {64, 128}; S <= 2^26; B * Hq * ceil(S / 32) < 2^24, in
- * the backward B * Hkv * sinks too; window >= 1, sinks >= 0; scale in [1e-20, 1e6]; tensors 16-byte aligned, with strides of
- * whole 16 bytes and row strides below 2^23 elements.
+ * Supported: D in {64, 128}; S <= 2^26; B * Hq * ceil(S / 32) < 2^24, in the
+ * backward also B * Hkv * sinks and B * Hkv * (ceil(S / 32) + ceil(sinks / 32));
+ * window >= 1, sinks >= 0; scale in [1e-20, 1e6]; tensors 16-byte aligned, with
+ * strides of whole 16 bytes and row strides below 2^23 elements.
  */
 cattn_status cattn_swa_fwd(const void* q, const void* k, const void* v, void* o, float* lse, const int* lens, int B,
                            int Hq, int Hkv, int S, int D, int window, int sinks, float scale,

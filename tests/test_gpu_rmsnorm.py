@@ -124,6 +124,23 @@ def test_a_replayed_graph_and_two_streams(cuda, rows, C):
         assert all(torch.equal(a, b) for a, b in zip(captured, want))
 
 
+def test_offsets_past_32_bits(cuda):
+    """2^31 elements and some: the last rows as a call of their own gives them."""
+    rows, C = (1 << 17) + 40, 16384
+    x = torch.zeros(rows, C, dtype=torch.bfloat16, device=cuda)
+    x[-40:] = randn(gen(60), 40, C, dtype="bf16").to(cuda)
+    gamma = torch.ones(C, device=cuda)
+    say(f"rmsnorm rows{rows} C{C}")
+    y, _, rstd = cattn.rmsnorm_fwd(x, gamma)
+    want, _, want_rstd = cattn.rmsnorm_fwd(x[-40:].contiguous(), gamma)
+    assert torch.equal(y[-40:], want) and torch.equal(rstd[-40:], want_rstd)
+    dx, _ = cattn.rmsnorm_bwd(x, gamma, rstd, x)
+    assert torch.equal(dx[-40:], cattn.rmsnorm_bwd(x[-40:].contiguous(), gamma, want_rstd, x[-40:].contiguous())[0])
+    q, scale, _, _ = cattn.rmsnorm_fwd_q8(x, gamma)
+    q40, scale40, _, _ = cattn.rmsnorm_fwd_q8(x[-40:].contiguous(), gamma)
+    assert torch.equal(q[-40:].view(torch.uint8), q40.view(torch.uint8)) and torch.equal(scale[-40:], scale40)
+
+
 def test_repeats_bit_for_bit_and_refuses(cuda):
     x, dy = randn(gen(5), 3000, 1600).to(cuda), randn(gen(6), 3000, 1600).to(cuda)
     gamma = torch.ones(1600, device=cuda)

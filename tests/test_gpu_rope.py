@@ -175,6 +175,18 @@ def test_more_tokens_than_one_grid_dimension_takes(cuda):
     assert int((o[0, 0, 1:] == 1).all(-1).sum()) <= 9  # ... at all: 9 angles have |sin| < 2e-7, whose row may be (1, 1) again
 
 
+def test_offsets_past_32_bits(cuda):
+    S, step = 600, 1 << 22
+    q = randn(gen(31), 1, 2, S, 64, dtype="bf16").to(cuda)
+    memory = torch.empty(S * step, dtype=q.dtype, device=cuda)
+    view = memory.as_strided((1, 2, S, 64), (128, 64, step, 1))
+    view.copy_(q)
+    f = cattn.rope_frequencies(32).to(cuda)
+    say("rope strides past 32 bits")
+    want, _ = cattn.rope_fwd(q, None, f)
+    assert torch.equal(cattn.rope_fwd(view, None, f, q_out=view)[0], want)
+
+
 def test_append_past_a_linear_cache_is_dropped(cuda):
     g = gen(9)
     q, k, v = (randn(g, 2, 1, 1, 64).to(cuda) for _ in range(3))

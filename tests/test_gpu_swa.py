@@ -189,6 +189,30 @@ def test_expanded_inputs_and_empty_sizes(cuda, dtype):
         assert o.shape == shape and lse.shape == shape[:3] and all(t.shape == shape for t in g)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_past_32_bits(cuda, dtype):
+    """Rows 2^22 elements apart, q, k, v, o and do side by side in them: the same bits as contiguous tensors give."""
+    S, step = 600, 1 << 22
+    t = inputs(9, 1, 2, 1, S, 64, dtype)
+    q, k, v, do = (x.to(cuda) for x in t)
+    memory = torch.empty(S * step, dtype=q.dtype, device=cuda)
+    at, views = 0, []
+    for x in (q, k, v, do, q):
+        heads = x.shape[1]
+        views.append(memory.as_strided((1, heads, S, 64), (heads * 64, 64, step, 1), at))
+        views[-1].copy_(x)
+        at += heads * 64
+    say(f"swa strides past 32 bits {dtype}")
+    o, lse = cattn.swa_fwd(q, k, v, 0.125, 90, 3)
+    got, got_lse = cattn.swa_fwd(*views[:3], 0.125, 90, 3, o=views[4])
+    assert torch.equal(got, o) and torch.equal(got_lse, lse)
+    want = cattn.swa_bwd(q, k, v, o, do, lse, 0.125, 90, 3)
+    dq = views[4]
+    o2 = o.clone()
+    got = cattn.swa_bwd(*views[:3], o2, views[3], lse, 0.125, 90, 3, dq=dq)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_repeats_and_streams(cuda):
     """The same bits every time, on another stream, and on two streams at once with workspaces of their own."""
     q, k, v, do = (t.to(cuda) for t in inputs(5, 2, 8, 2, 700, 64, "bf16"))
