@@ -389,7 +389,7 @@ cattn_status cattn_rope_frequencies(double* freqs, int rot, double base, int sca
  *   freqs:    DEVICE double [rot / 2]
  * Supported: D even, 2 .. 512; rot even, 2 .. D; B * S < 2^31 - 1.  Any strides and
  * element-aligned addresses; 16-byte ones with rot / 2 (interleaved: rot) and
- * D - rot multiples of 16 bytes are the fast path.
+ * D - rot multiples of 16 bytes are the fast path, of 8 the next.
  */
 cattn_status cattn_rope(const void* q, const void* k, void* q_out, void* k_out, const int* positions,
                         const double* freqs, int B, int S, int Hq, int Hkv, int D, int rot, int batched,

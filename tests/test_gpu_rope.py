@@ -31,6 +31,7 @@ CASES = [  # B, Hq, Hkv, S, D, rot, interleaved, layout
     (1, 8, 2, 17, 128, 24, False, "bhsd"), (3, 2, 2, 7, 64, 6, True, "bshd"), (1, 5, 5, 3, 70, 70, False, "bhsd"),
     (2, 40, 8, 9, 128, 64, True, "bshd"), (1, 2, 1, 4, 512, 512, False, "bhsd"), (1, 1, 1, 3, 512, 2, True, "bhsd"),
     (4, 12, 4, 700, 64, 64, False, "bhsd"), (2, 4, 4, 6000, 64, 48, False, "bshd"), (1, 300, 20, 2, 16, 8, False, "bhsd"),
+    (2, 4, 2, 30, 128, 20, True, "bhsd"), (2, 4, 2, 300, 64, 24, False, "bshd"),
 ]
 
 
