@@ -777,13 +777,14 @@ template <int ROWS> dim3 rows_grid(const SwaArgs& a, int heads) {
 //          g 2    F 14.0 / 9.6 / 15.3, K 33.2 / 28.3 / 35.6 (1024, 128); K 8/2 424 / 288 / 341 / 357 (8192, 2048)
 //          g 4    F 14.8 / 12.2, Q 37.0 / 38.0, K 36.8 / 42.5 / - / 38.8 (1024, 128); F 22.6 / 17.4, Q 58.5 / 56.8, K
 //                 58.2 / 65.3 / - / 57.1 (1024, 512); K 16/4 293 / 313 / - / 264 (8192, 1024)
-//          g 5    F 29.6 / 27.8 (5000, 512), 57.6 / 49.8 (5000, 2048); K 76.8 / 79.7 / - / 91.4 (5000, 512)
+//          g 5    F 15.5 / 17.6 (5000, 8), 21.4 / 22.0 (5000, 200), 29.6 / 27.8 (5000, 512), 57.6 / 49.8 (5000, 2048);
+//                 K 76.8 / 79.7 / - / 91.4 (5000, 512)
 //          g 6    F 19.9 / 19.3 (1024, 128), 109 / 117 (8192, 4096); Q 319 / 341, K 321 / 364 / - / 345 (8192, 4096)
 enum Form { kWhole = 1, kTwo = 2, kFour = 4, kEight = 8 };
 Form form_of(Pass pass, int D, int64_t heads, int S, int run) {
   const int64_t groups = heads * ((S + 31) / 32), cus = cu_count();
   if (groups <= cus || (D == 64 && groups <= 2 * cus && run >= 16)) return kFour;
-  if (groups > (D == 128 && pass == Pass::kFwd ? 5 : 4) * cus) return kWhole;
+  if (groups > (D == 128 && pass == Pass::kFwd && run >= 16 ? 5 : 4) * cus) return kWhole;
   if (D == 64 || pass == Pass::kFwd || groups <= 2 * cus) return kTwo;
   if (run < 16) return kWhole;
   return pass == Pass::kDq ? kTwo : kEight;
