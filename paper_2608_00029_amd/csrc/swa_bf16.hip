@@ -49,6 +49,7 @@ namespace cattn {
 
 namespace {
 
+constexpr int W = 4;  // waves of a work group
 constexpr float kSumMax = 4294967296.0f;  // bound of a block's probability sum before the offset moves
 
 // dma16 to LDS byte address lds + OFF: the sum is formed in M0, so that the many
@@ -62,17 +63,16 @@ template <int OFF> __device__ __forceinline__ void dma16_at(const void* sbase, u
 #pragma clang diagnostic pop
 
 // HBM -> LDS copies of pairs of 32-row tiles (K and V, or Q and dO) by a work
-// group of W waves, in 1 KB pieces, every wave some of both tiles.  A lane's
+// group's four waves, in 1 KB pieces, every wave some of both tiles.  A lane's
 // offsets inside a tile are fixed for the kernel; a tile that reaches past the
 // sequence's end, whose rows past row `last` repeat it, forms its own.  (Row
 // strides stay below 2^23: 24-bit products.)  TIGHT, for dK/dV at D = 128, whose
 // registers are all in use: one register per tensor and one for the chunk instead
 // of two per tensor, an addition of three terms per copy.
-template <int D, int W, bool TIGHT = false> struct SwaCopy {
+template <int D, bool TIGHT = false> struct SwaCopy {
   static constexpr int TILE = TileGeom<D>::TILE, PIECES = TILE / 1024, CPR = TileGeom<D>::CPR;
   static constexpr int N = PIECES / W, STEP = 64 * W / CPR;
   static constexpr int PER_PAIR = 2 * N;  // copies of each wave
-  static_assert(PIECES % W == 0, "whole pieces");
   static_assert(!TIGHT || (N == 2 && STEP == 16), "the second copy's rows are 16 on: swz(row + 16) = swz(row) ^ 7");
   unsigned va[TIGHT ? 1 : N], vb[TIGHT ? 1 : N];  // byte offsets of this lane's chunks; TIGHT: of its row
   unsigned chunk;                                 // TIGHT: the chunk's offset in the row
@@ -126,8 +126,8 @@ template <int D, int W, bool TIGHT = false> struct SwaCopy {
 
 // The key and value tiles of a work group, copied in order: a running pointer to
 // each, moved by a tile's rows, and once from the sinks to the window.
-template <int D, int W> struct KeyStream {
-  SwaCopy<D, W> tc;
+template <int D> struct KeyStream {
+  SwaCopy<D> tc;
   const bf16 *k, *v;
   int64_t dk, dv, jump_k, jump_v;
   int x, n, sink_tiles, last;  // next tile; `last`: the last row of the last tile, below 31 if that is ragged
@@ -217,14 +217,14 @@ template <int D> __device__ __forceinline__ int acc_col(int dt, int g, int h) { 
 
 // ---------------------------------------------------------------------------
 // Forward.  A work group owns 32 * QG queries of one head and takes its key
-// tiles in SPLIT interleaved parts by W = QG * SPLIT waves.
+// tiles in SPLIT interleaved parts by QG * SPLIT = 4 waves.
 // ---------------------------------------------------------------------------
-template <int D, int W, int SPLIT, int NB>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 128 ? 3 : 4, 10)))
+template <int D, int SPLIT, int NB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 128 ? 3 : 4, 10)))
 void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   typedef TileGeom<D> G;
   constexpr int QG = W / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
-  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_SLOT = SPLIT * SwaCopy<D, W>::PER_PAIR;
+  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_SLOT = SPLIT * SwaCopy<D>::PER_PAIR;
   __shared__ __attribute__((aligned(16))) char smem[SPLIT * NB * SET];  // [part][slot][K, V]
   __shared__ float stats[2][W][SPLIT > 1 ? 64 : 1];
   static_assert(SPLIT == 1 || W * 64 * DT * 16 * 4 <= SPLIT * NB * SET, "merge area");
@@ -258,7 +258,7 @@ void swa_fwd_bf16_kernel(SwaArgs a, float c) {
 
   const KeyTiles kt(q0, min(len, q0 + BQ), a.window, a.sinks);
   const int L = (kt.n + SPLIT - 1) / SPLIT;
-  KeyStream<D, W> keys;
+  KeyStream<D> keys;
   keys.init(a, kt, b, hk, len, smem, w);
   auto dma = [&](int, auto slc) __attribute__((always_inline)) {  // the next iteration's tile of every part
     unroll<SPLIT>([&](auto p) __attribute__((always_inline)) { keys.template copy<(decltype(p)::value * NB + decltype(slc)::value) * SET>(); });
@@ -406,12 +406,12 @@ __device__ __forceinline__ void sum_parts(f32x4* area, int w, int h, int lane, c
 // past the sequence's end) into the workspace for the dK/dV kernels.  The dP
 // contraction starts from D and multiplies by -dO, so it yields D - dP.
 // ---------------------------------------------------------------------------
-template <int D, int W, int SPLIT, int NB>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 64 ? 4 : 2, 10)))
+template <int D, int SPLIT, int NB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 64 ? 4 : 2, 10)))
 void swa_dq_bf16_kernel(SwaArgs a, float c) {
   typedef TileGeom<D> G;
   constexpr int QG = W / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
-  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_SLOT = SPLIT * SwaCopy<D, W>::PER_PAIR;
+  constexpr int TILE = G::TILE, SET = 2 * TILE, PER_SLOT = SPLIT * SwaCopy<D>::PER_PAIR;
   __shared__ __attribute__((aligned(16))) char smem[SPLIT * NB * SET];  // [part][slot][K, V]
   static_assert(SPLIT == 1 || W * 64 * DT * 16 * 4 <= SPLIT * NB * SET, "merge area");
   static_assert(NB * SET <= 65536, "tile reads reach every slot by immediate offset");
@@ -440,7 +440,7 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
 
   const KeyTiles kt(q0, min(len, q0 + BQ), a.window, a.sinks);
   const int L = (kt.n + SPLIT - 1) / SPLIT;
-  KeyStream<D, W> keys;
+  KeyStream<D> keys;
   keys.init(a, kt, b, hk, len, smem, w);
   auto dma = [&](int, auto slc) __attribute__((always_inline)) {  // the next iteration's tile of every part
     unroll<SPLIT>([&](auto p) __attribute__((always_inline)) { keys.template copy<(decltype(p)::value * NB + decltype(slc)::value) * SET>(); });
@@ -524,20 +524,19 @@ void swa_dq_bf16_kernel(SwaArgs a, float c) {
 // ---------------------------------------------------------------------------
 // Backward, kernel 2: dK, dV.  A work group owns 32 * KG keys of one key/value
 // head and walks, for each query head of the group, the query tiles that see
-// them from the last down, in SPLIT interleaved parts by W = KG * SPLIT waves.  A far
+// them from the last down, in SPLIT interleaved parts by KG * SPLIT = 4 waves.  A far
 // work group takes the pairs that only the sinks see, 32 sink keys and one part of
 // the walk, into the far area, the others the pairs of the window.  Where both fit
 // one form they may share a grid (swa_far_shares), the first n_far work groups far.
 // ---------------------------------------------------------------------------
 enum class Pairs { kWindow, kFar, kBoth };
-template <int D, int W, int SPLIT, int NB, Pairs PAIRS>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 8 ? 2 : SPLIT > 1 ? 1 : D == 64 ? 3 : 2, 10)))
+template <int D, int SPLIT, int NB, Pairs PAIRS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 64 ? 3 : 2, 10)))
 void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts, int n_far) {
   typedef TileGeom<D> G;
   constexpr int KG = W / SPLIT, BKV = 32 * KG, KS_D = D / 16, DT = D / 32;
   constexpr int TILE = G::TILE, SETB = 2 * TILE, AUX = 2 * 32 * 4, AUX0 = SPLIT * NB * SETB;
-  constexpr int AUX_COPIES = 4 * SPLIT / W, PER_SLOT = SPLIT * SwaCopy<D, W>::PER_PAIR + AUX_COPIES;
-  static_assert(AUX_COPIES * W == 4 * SPLIT, "four waves copy a part's workspace rows");
+  constexpr int PER_SLOT = SPLIT * (SwaCopy<D>::PER_PAIR + 1);
   // [part][slot] Q, dO tiles, then [part][slot] -LSE/scale and D rows
   __shared__ __attribute__((aligned(16))) char smem[SPLIT * NB * (SETB + AUX)];
   static_assert(SPLIT == 1 || W * 64 * DT * 16 * 4 <= SPLIT * NB * SETB, "merge area");
@@ -570,10 +569,10 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts, int n_far) {
   }
   const int L = (n + SPLIT - 1) / SPLIT;
 
-  SwaCopy<D, W, D == 128 && W == 4> tc;
+  SwaCopy<D, D == 128> tc;
   tc.init(smem, w, a.sq.s, a.sdo.s);
   // a part's 8 chunks of -LSE/scale and 8 of D: lanes 0..3 of four waves
-  const int ldq = 4 * (w & 3) + (lane & 3);
+  const int ldq = 4 * w + (lane & 3);
   const unsigned ld_voff = (unsigned)((ldq < 8 ? Sp + 4 * ldq : 4 * (ldq - 8)) * 4);
   // The walk: position x is query tile jhi - x % nj of head x / nj.  Running
   // pointers to the next position to copy, moved up a tile, or to the last tile
@@ -588,13 +587,13 @@ void swa_dkdv_bf16_kernel(SwaArgs a, float c, int far_parts, int n_far) {
   const int64_t up_q = 32 * a.sq.s, up_do = 32 * a.sdo.s;
   const int64_t next_q = a.sq.h + back * a.sq.s, next_do = a.sdo.h + back * a.sdo.s, next_ws = 2 * (int64_t)Sp + back;
   const int jrag = len % 32 ? len / 32 : -1;  // the tile that reaches past the end
-  const unsigned aux_lds = lds_addr(smem) + 64 * (w & 3);
+  const unsigned aux_lds = lds_addr(smem) + 64 * w;
   auto dma = [&](int, auto slc) __attribute__((always_inline)) {
     unroll<SPLIT>([&](auto p_) __attribute__((always_inline)) {
       constexpr int p = decltype(p_)::value, slot = p * NB + decltype(slc)::value;
       if (j != jrag) tc.template pair<slot * SETB>(qp, dop);
       else tc.template pair_last<slot * SETB>(qp, dop, len % 32 - 1);
-      if ((W == 4 || w / 4 == p) && lane < 4) dma16_at<AUX0 + slot * AUX>(wsp, ld_voff, aux_lds);
+      if (lane < 4) dma16_at<AUX0 + slot * AUX>(wsp, ld_voff, aux_lds);
       if (SPLIT > 1 && ++pos >= n) return;  // (a part without a tile copies the last again)
       qp -= up_q;
       dop -= up_do;
@@ -760,71 +759,69 @@ template <int ROWS> dim3 rows_grid(const SwaArgs& a, int heads) {
   return dim3((unsigned)((int64_t)a.B * heads * ((a.S + ROWS - 1) / ROWS)));
 }
 
-// How a kernel's work groups divide their walk over the other axis: not (128
-// rows, four waves), in two parts (64 rows), in four (32 rows), or in two parts by
-// eight waves (128 rows).  A grid of few 128-row work groups leaves CUs idle and
-// its waves the whole walk; more parts cost rings, LDS and the parts' merge.  What
-// decides are the 32-row groups per CU, g, and `run`, the tiles a work group walks
-// (of all heads of the group in dK/dV).  Measured, none / two / four parts / eight
-// waves, us (MHA unless Hq/Hkv; F forward, Q dQ, K dK/dV with the other kernel's
-// time in; S, window):
+// How a kernel's work groups divide their walk over the other axis: not (128 rows
+// of four waves), in two parts (64 rows) or in four (32 rows).  A grid of few
+// 128-row work groups leaves CUs idle and its waves the whole walk; more parts cost
+// rings, LDS and the parts' merge.  What decides are the 32-row groups per CU, g, and
+// `run`, the tiles a work group walks (of all heads of the group in dK/dV).
+// Measured, none / two / four parts, us (MHA unless Hq/Hkv; F forward, Q dQ, K dK/dV
+// with the other kernel's time in; S, window):
 //   D  64  g 1    F 15.5 / 10.5 / 9.0 (1024, 512), K 180 / 144 / 123 (8192, 4096)
 //          g 2    F 9.7 / 8.7 / 8.8, K 23.0 / 20.2 / 20.7 (1024, 128); F 15.5 / 10.7 / 9.9, K 38.3 / 32.2 / 30.7
 //                 (1024, 512); K 8/2 267 / 188 / 176 (8192, 2048)
 //          g 4    F 15.9 / 12.8 / 16.7, K 39.1 / 36.0 / 40.8 (1024, 512); K 16/4 183 / 161 / 185 (8192, 1024)
 //          g 6    F 12.0 / 13.6, K 30.5 / 32.5 (1024, 128); F 69.1 / 71.8, K 190 / 199 (8192, 4096)
 //   D 128  g 1    F 22.0 / 13.5 / 11.4, K 55.7 / 45.1 / 40.7 (1024, 512)
-//          g 2    F 14.0 / 9.6 / 15.3, K 33.2 / 28.3 / 35.6 (1024, 128); K 8/2 424 / 288 / 341 / 357 (8192, 2048)
-//          g 4    F 14.8 / 12.2, Q 37.0 / 38.0, K 36.8 / 42.5 / - / 38.8 (1024, 128); F 22.6 / 17.4, Q 58.5 / 56.8, K
-//                 58.2 / 65.3 / - / 57.1 (1024, 512); K 16/4 293 / 313 / - / 264 (8192, 1024)
+//          g 2    F 14.0 / 9.6 / 15.3, K 33.2 / 28.3 / 35.6 (1024, 128); K 8/2 424 / 288 / 341 (8192, 2048)
+//          g 3    Q 53.3 / 56.1, K 54.5 / 49.4 (1152, 40/20, 130); Q 71.2 / 64.8, K 70.0 / 59.2 (1024, 1024);
+//                 Q 370 / 365, K 458 / 365 (6144, 16/4, 2048)
+//          g 4    F 14.8 / 12.2, Q 36.3 / 37.3, K 35.8 / 35.6 (1024, 128); F 22.6 / 17.4, Q 55.3 / 54.5, K 55.6 / 51.8
+//                 (1024, 512); Q 252 / 264, K 281 / 253 (8192, 16/4, 1024)
 //          g 5    F 15.5 / 17.6 (5000, 8), 21.4 / 22.0 (5000, 200), 29.6 / 27.8 (5000, 512), 57.6 / 49.8 (5000, 2048);
-//                 K 76.8 / 79.7 / - / 91.4 (5000, 512)
-//          g 6    F 19.9 / 19.3 (1024, 128), 109 / 117 (8192, 4096); Q 319 / 341, K 321 / 364 / - / 345 (8192, 4096)
-enum Form { kWhole = 1, kTwo = 2, kFour = 4, kEight = 8 };
+//                 K 76.8 / 79.7 (5000, 512)
+//          g 6    F 19.9 / 19.3 (1024, 128), 109 / 117 (8192, 4096); Q 319 / 341, K 321 / 364 (8192, 4096)
+enum Form { kWhole = 1, kTwo = 2, kFour = 4 };
 Form form_of(Pass pass, int D, int64_t heads, int S, int run) {
   const int64_t groups = heads * ((S + 31) / 32), cus = cu_count();
   if (groups <= cus || (D == 64 && groups <= 2 * cus && run >= 16)) return kFour;
   if (groups > (D == 128 && pass == Pass::kFwd && run >= 16 ? 5 : 4) * cus) return kWhole;
-  if (D == 64 || pass == Pass::kFwd || groups <= 2 * cus) return kTwo;
-  if (run < 16) return kWhole;
-  return pass == Pass::kDq ? kTwo : kEight;
+  if (D == 128 && pass == Pass::kDq && groups > 2 * cus && run < 16) return kWhole;
+  return kTwo;
 }
 // Tiles that a work group of 128 rows walks on one head.
 int run_of(const SwaArgs& a) {
   return std::min((a.S + 31) / 32, (std::min(a.window, a.S) + 127) / 32 + swa_sink_tiles(a.S, a.sinks));
 }
 
-template <int D, int W, int SPLIT, int NB> hipError_t fwd_s(const SwaArgs& a, float c, hipStream_t st) {
-  hipLaunchKernelGGL((swa_fwd_bf16_kernel<D, W, SPLIT, NB>), rows_grid<32 * W / SPLIT>(a, a.Hq), dim3(64 * W), 0, st, a,
-                     c);
+template <int D, int SPLIT, int NB> hipError_t fwd_s(const SwaArgs& a, float c, hipStream_t st) {
+  hipLaunchKernelGGL((swa_fwd_bf16_kernel<D, SPLIT, NB>), rows_grid<128 / SPLIT>(a, a.Hq), dim3(256), 0, st, a, c);
   return hipGetLastError();
 }
-template <int D, int W, int SPLIT, int NB> hipError_t dq_s(const SwaArgs& a, float c, hipStream_t st) {
-  hipLaunchKernelGGL((swa_dq_bf16_kernel<D, W, SPLIT, NB>), rows_grid<32 * W / SPLIT>(a, a.Hq), dim3(64 * W), 0, st, a,
-                     c);
+template <int D, int SPLIT, int NB> hipError_t dq_s(const SwaArgs& a, float c, hipStream_t st) {
+  hipLaunchKernelGGL((swa_dq_bf16_kernel<D, SPLIT, NB>), rows_grid<128 / SPLIT>(a, a.Hq), dim3(256), 0, st, a, c);
   return hipGetLastError();
 }
-template <int D, int W, int SPLIT, int NB> hipError_t dkdv_s(const SwaArgs& a, float c, int far, hipStream_t st) {
-  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, W, SPLIT, NB, Pairs::kWindow>), rows_grid<32 * W / SPLIT>(a, a.Hkv),
-                     dim3(64 * W), 0, st, a, c, far, 0);
+template <int D, int SPLIT, int NB> hipError_t dkdv_s(const SwaArgs& a, float c, int far, hipStream_t st) {
+  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, SPLIT, NB, Pairs::kWindow>), rows_grid<128 / SPLIT>(a, a.Hkv), dim3(256), 0,
+                     st, a, c, far, 0);
   return hipGetLastError();
 }
 
 template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
   switch (form_of(Pass::kFwd, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
-    case kFour: return fwd_s<D, 4, 4, 2>(a, c, st);
-    case kTwo: return fwd_s<D, 4, 2, D == 64 ? 4 : 2>(a, c, st);
-    default: return fwd_s<D, 4, 1, D == 64 ? 4 : 3>(a, c, st);
+    case kFour: return fwd_s<D, 4, 2>(a, c, st);
+    case kTwo: return fwd_s<D, 2, D == 64 ? 4 : 2>(a, c, st);
+    default: return fwd_s<D, 1, D == 64 ? 4 : 3>(a, c, st);
   }
 }
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
   hipError_t e;
   switch (form_of(Pass::kDq, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
-    case kFour: e = dq_s<D, 4, 4, 2>(a, c, st); break;
-    case kTwo: e = dq_s<D, 4, 2, D == 64 ? 4 : 2>(a, c, st); break;
-    default: e = dq_s<D, 4, 1, 4>(a, c, st);
+    case kFour: e = dq_s<D, 4, 2>(a, c, st); break;
+    case kTwo: e = dq_s<D, 2, D == 64 ? 4 : 2>(a, c, st); break;
+    default: e = dq_s<D, 1, 4>(a, c, st);
   }
   if (e != hipSuccess) return e;
   const Form form = form_of(Pass::kDkdv, D, (int64_t)a.B * a.Hkv, a.S, run_of(a) * (a.Hq / a.Hkv));
@@ -834,23 +831,18 @@ template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   switch (form) {
     case kFour:
       if (far && shared) {
-        hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 4, 2, Pairs::kBoth>), dim3(n_far + rows_grid<32>(a, a.Hkv).x),
+        hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 2, Pairs::kBoth>), dim3(n_far + rows_grid<32>(a, a.Hkv).x),
                            dim3(256), 0, st, a, c, far, n_far);
         e = hipGetLastError();
         return e != hipSuccess ? e : launch_swa_far_sum(a, far, st);
       }
-      e = dkdv_s<D, 4, 4, 2>(a, c, far, st);
+      e = dkdv_s<D, 4, 2>(a, c, far, st);
       break;
-    case kTwo: e = dkdv_s<D, 4, 2, D == 64 ? 4 : 2>(a, c, far, st); break;
-    case kEight:
-      if constexpr (D == 128) {
-        e = dkdv_s<D, 8, 2, 4>(a, c, far, st);
-        break;
-      }
-    default: e = dkdv_s<D, 4, 1, 4>(a, c, far, st);
+    case kTwo: e = dkdv_s<D, 2, D == 64 ? 4 : 2>(a, c, far, st); break;
+    default: e = dkdv_s<D, 1, 4>(a, c, far, st);
   }
   if (e != hipSuccess || !far) return e;
-  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 4, 2, Pairs::kFar>), dim3(n_far), dim3(256), 0, st, a, c, far, n_far);
+  hipLaunchKernelGGL((swa_dkdv_bf16_kernel<D, 4, 2, Pairs::kFar>), dim3(n_far), dim3(256), 0, st, a, c, far, n_far);
   e = hipGetLastError();
   return e != hipSuccess ? e : launch_swa_far_sum(a, far, st);
 }
