@@ -34,10 +34,10 @@
 // cycles of the matrix cores and about 500 of vector instructions, half of them
 // the 16 exponentials; it measures 600 with three waves per SIMD.  Small grids and
 // narrow windows are bound by the first tiles' way from HBM (B8 H12 S1024 D64,
-// forward / backward, us: window 1 12.4 / 31.9, 256 19.5 / 49.9, 1024 24.8 / 69.7; q,
+// forward / backward, us: window 1 12.4 / 31.4, 256 17.5 / 46.1, 1024 22.7 / 64.7; q,
 // k, v and o alone take 10 at 5.15 TB/s).  Measured, B2 H16 S8192 D128, TFLOP/s of 4 D
-// / 10 D operations per visible pair: window 512 608 / 485, 1024 814 / 628, 4096
-// 1009 / 761, no window 1081 / 800 (causal kernels: 1108 / 830).
+// / 10 D operations per visible pair: window 512 623 / 508, 1024 838 / 639, 4096
+// 1051 / 802, no window 1116 / 841 (causal kernels: 1144 / 866).
 #include <algorithm>
 #include <utility>
 
