@@ -220,7 +220,7 @@ template <int D> __device__ __forceinline__ int acc_col(int dt, int g, int h) { 
 // tiles in SPLIT interleaved parts by QG * SPLIT = 4 waves.
 // ---------------------------------------------------------------------------
 template <int D, int SPLIT, int NB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 128 ? 3 : 4, 10)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SPLIT > 1 ? 1 : D == 64 ? 4 : NB == 3 ? 3 : 2, 10)))
 void swa_fwd_bf16_kernel(SwaArgs a, float c) {
   typedef TileGeom<D> G;
   constexpr int QG = W / SPLIT, BQ = 32 * QG, KS_D = D / 16, DT = D / 32;
@@ -812,8 +812,14 @@ template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
   switch (form_of(Pass::kFwd, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
     case kFour: return fwd_s<D, 4, 2>(a, c, st);
     case kTwo: return fwd_s<D, 2, D == 64 ? 4 : 2>(a, c, st);
-    default: return fwd_s<D, 1, D == 64 ? 4 : 3>(a, c, st);
+    default: break;
   }
+  // A ring of four (a barrier every second tile) holds two work groups of D = 128 a
+  // CU, one of three holds three: better from the third on (four / three, us: B4 H12
+  // S1024 window 256, 384 work groups, 22.6 / 24.3; B1 H16 S4096 window 4096, 512, 99.8
+  // / 102.8; B1 H12 S8192 window 1024, 768, 77.9 / 73.1).
+  const bool two = (int64_t)a.B * a.Hq * ((a.S + 127) / 128) <= 2 * (int64_t)cu_count();
+  return D == 64 || two ? fwd_s<D, 1, 4>(a, c, st) : fwd_s<D, 1, 3>(a, c, st);
 }
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
