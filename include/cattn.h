@@ -337,7 +337,9 @@ cattn_status cattn_rmsnorm_fwd(const void* x, const void* residual, const float*
  * and scale [rows, ceil(C / group)] their float scales, one per `group`
  * consecutive columns of a row (the last group may be shorter; group 0: one
  * per row):
- *     scale = max(max|y| / 448, 2^-126),  q = e4m3(y / scale)   (to nearest even)
+ *     scale = max(max|y| / 448, 2^-126),  q = e4m3(y / scale)
+ * The quotient is float32 (exact to 2^-46 before that rounding), and it rounds to
+ * the nearest code, from the middle of two to the even one.
  * A NaN of y stays one in q.  group: 0, or a power of two from 8 to 512
  * (CATTN_ERR_INVALID_ARG otherwise).  q is 16-byte aligned, scale 4-byte. */
 cattn_status cattn_rmsnorm_fwd_q8(const void* x, const void* residual, const float* gamma, unsigned char* q,
