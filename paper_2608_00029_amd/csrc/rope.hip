@@ -13,6 +13,7 @@
 #include "attn_device.h"
 #include "attn_launch.h"
 #include "block_launch.h"
+#include "row_access.h"
 
 namespace cattn {
 
@@ -20,48 +21,6 @@ namespace {
 
 constexpr int kMaxTokens = 8;     // tokens of a work group
 constexpr int kRopeTable = 256;   // (token, pair) entries of its table
-
-// V consecutive elements; 16 or 8 bytes' worth is one access.
-template <int V> struct Floats { typedef float type __attribute__((ext_vector_type(V))); };
-template <typename T, int V> __device__ __forceinline__ typename Floats<V>::type load_v(const T* p) {
-  typename Floats<V>::type f;
-  if constexpr (sizeof(T) == 2 && V == 8) {
-    const bf16x8 v = *(const bf16x8*)p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
-  } else if constexpr (sizeof(T) == 2 && V == 4) {
-    const bf16x4 v = *(const bf16x4*)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = (float)v[e];
-  } else if constexpr (sizeof(T) == 4 && V == 4) {
-    f = *(const f32x4*)p;
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = (float)p[e];
-  }
-  return f;
-}
-template <typename T, int V, bool NT = false>
-__device__ __forceinline__ void store_v(T* p, typename Floats<V>::type f) {
-  if constexpr (V * sizeof(T) >= 8) {
-    typedef unsigned words __attribute__((ext_vector_type(V * sizeof(T) / 4)));
-    words u;
-    if constexpr (sizeof(T) == 2) {
-      typedef __bf16 halves __attribute__((ext_vector_type(V)));
-      halves v;
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = (__bf16)f[e];
-      u = __builtin_bit_cast(words, v);
-    } else {
-      u = __builtin_bit_cast(words, f);
-    }
-    if constexpr (NT) __builtin_nontemporal_store(u, (words*)p);
-    else *(words*)p = u;
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) p[e] = (T)f[e];
-  }
-}
 
 // (field by field: a choice between two structs would go through memory)
 __device__ __forceinline__ Strides choose(bool first, const Strides& x, const Strides& y) {
