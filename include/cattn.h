@@ -306,7 +306,8 @@ cattn_status cattn_sce_bwd(const float* logits, const int* targets, const float*
  * sliding-window attention, in training and for single tokens.  They follow the
  * conventions above (device pointers, asynchronous on `stream`, no allocation,
  * no state, deterministic, argument errors before anything is enqueued) with
- * these differences.
+ * these differences.  The *_workspace_bytes functions give 0 for an empty, invalid
+ * or unsupported shape.
  *
  * Query and key/value heads may be grouped: Hq a multiple of Hkv, and query
  * head h reads key/value head h / (Hq / Hkv).

@@ -152,7 +152,7 @@ static cattn_status rmsnorm_fwd(const void* x, const void* residual, const float
     return fail(CATTN_ERR_INVALID_ARG, "group must be 0 or a power of two from 8 to 512");
   if (rows == 0 || C == 0) return CATTN_OK;
   if (C % 8 || C > kRmsMaxC) return fail(CATTN_ERR_UNSUPPORTED, "C must be a multiple of 8 and at most 16384");
-  if (rows > (1 << 30)) return fail(CATTN_ERR_UNSUPPORTED, "rows exceeds 2^30");
+  if (rows > kRmsMaxRows) return fail(CATTN_ERR_UNSUPPORTED, "rows exceeds 2^30");
   if (!x || !gamma || !y || !rstd || (q8 && !scale)) return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");
   if (!residual != !h) return fail(CATTN_ERR_INVALID_ARG, "h goes with a residual");
   for (const void* p : {x, residual, (const void*)gamma, (const void*)y, (const void*)h})
@@ -182,7 +182,7 @@ cattn_status cattn_rmsnorm_fwd_q8(const void* x, const void* residual, const flo
 }
 
 size_t cattn_rmsnorm_bwd_workspace_bytes(int rows, int C) {
-  if (rows <= 0 || C <= 0) return 0;
+  if (rows <= 0 || C <= 0 || rows > kRmsMaxRows || C > kRmsMaxC || C % 8) return 0;
   return (size_t)rms_bwd_groups(rows, C) * (size_t)C * sizeof(float);
 }
 
@@ -193,7 +193,7 @@ cattn_status cattn_rmsnorm_bwd(const void* h, const float* gamma, const float* r
   if (!valid_dtype(dtype)) return fail(CATTN_ERR_INVALID_ARG, "dtype must be CATTN_F32 or CATTN_BF16");
   if (rows == 0 || C == 0) return CATTN_OK;
   if (C % 8 || C > kRmsMaxC) return fail(CATTN_ERR_UNSUPPORTED, "C must be a multiple of 8 and at most 16384");
-  if (rows > (1 << 30)) return fail(CATTN_ERR_UNSUPPORTED, "rows exceeds 2^30");
+  if (rows > kRmsMaxRows) return fail(CATTN_ERR_UNSUPPORTED, "rows exceeds 2^30");
   if (!h || !gamma || !rstd || !dy || !dx || !dgamma || !workspace)
     return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");
   for (const void* p : {h, (const void*)gamma, dy, dh, (const void*)dx, (const void*)dgamma, (const void*)workspace})
@@ -339,6 +339,16 @@ cattn_status cattn_rope_append(const void* q, const void* k, const void* v, void
 // ---------------------------------------------------------------------------
 // Work groups that a launch may have: their threads (256 each) are counted in 32 bits.
 constexpr int64_t kMaxGroups = 1 << 24;
+constexpr int kMaxS = 1 << 26;
+
+// Whether sizes that are consistent are within the limits of every pass, and of the backward.
+static bool swa_D(int D) { return D == 64 || D == 128; }
+static bool swa_fits(int B, int Hq, int S) { return S <= kMaxS && (int64_t)B * Hq < kMaxGroups; }
+static bool swa_bwd_fits(int B, int Hq, int Hkv, int S, int sinks) {
+  const int64_t tiles = ((int64_t)S + 31) / 32, heads = (int64_t)B * Hkv;  // (Hkv <= Hq)
+  return swa_fits(B, Hq, S) && (int64_t)B * Hq * tiles < kMaxGroups && heads * (tiles + swa_sink_tiles(S, sinks)) < kMaxGroups &&
+         heads * std::min(sinks, S) < kMaxGroups;
+}
 
 static cattn_status swa_sizes(int B, int Hq, int Hkv, int S, int D, int window, int sinks, float scale, int layout,
                               int dtype, bool* empty) {
@@ -349,14 +359,14 @@ static cattn_status swa_sizes(int B, int Hq, int Hkv, int S, int D, int window, 
   if (!valid_dtype(dtype)) return fail(CATTN_ERR_INVALID_ARG, "dtype must be CATTN_F32 or CATTN_BF16");
   if (!(scale >= kMinScale && scale <= kMaxScale)) return fail(CATTN_ERR_INVALID_ARG, "scale must lie in [1e-20, 1e6]");
   if (window < 1 || sinks < 0) return fail(CATTN_ERR_INVALID_ARG, "window must be at least 1 and sinks at least 0");
-  if (D != 64 && D != 128) return fail(CATTN_ERR_UNSUPPORTED, "head dimension D must be 64 or 128");
+  if (!swa_D(D)) return fail(CATTN_ERR_UNSUPPORTED, "head dimension D must be 64 or 128");
   if (B == 0 || S == 0 || (Hq == 0 && Hkv == 0)) {
     *empty = true;
     return CATTN_OK;
   }
   if (Hq == 0 || Hkv == 0 || Hq % Hkv) return fail(CATTN_ERR_INVALID_ARG, "Hq must be a multiple of Hkv");
-  if (S > (1 << 26)) return fail(CATTN_ERR_UNSUPPORTED, "S (cap) exceeds 2^26");
-  if ((int64_t)B * Hq >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
+  if (S > kMaxS) return fail(CATTN_ERR_UNSUPPORTED, "S (cap) exceeds 2^26");
+  if (!swa_fits(B, Hq, S)) return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
   return CATTN_OK;
 }
 
@@ -399,7 +409,8 @@ cattn_status cattn_swa_fwd(const void* q, const void* k, const void* v, void* o,
 }
 
 size_t cattn_swa_bwd_workspace_bytes(int B, int Hq, int Hkv, int S, int D, int window, int sinks) {
-  if (B <= 0 || Hq <= 0 || Hkv <= 0 || S <= 0 || D <= 0 || window < 1 || sinks < 0 || Hq % Hkv) return 0;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || S <= 0 || !swa_D(D) || window < 1 || sinks < 0 || Hq % Hkv) return 0;
+  if (!swa_bwd_fits(B, Hq, Hkv, S, sinks)) return 0;
   const int w = std::min(window, S), k = std::min(sinks, S);
   return sizeof(float) * (2 * (size_t)B * Hq * (size_t)ws_rows(S) + (size_t)swa_far_floats(B, Hq, Hkv, S, D, w, k));
 }
@@ -412,10 +423,7 @@ cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const vo
   bool empty;
   cattn_status st = swa_sizes(B, Hq, Hkv, S, D, window, sinks, scale, layout, dtype, &empty);
   if (st != CATTN_OK || empty) return st;
-  if ((int64_t)B * Hq * ((S + 31) / 32) >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
-  if ((int64_t)B * Hkv * ((S + 31) / 32 + swa_sink_tiles(S, sinks)) >= kMaxGroups)
-    return fail(CATTN_ERR_UNSUPPORTED, "grid too large");
-  if ((int64_t)B * Hkv * std::min(sinks, S) >= kMaxGroups) return fail(CATTN_ERR_UNSUPPORTED, "too many sinks");
+  if (!swa_bwd_fits(B, Hq, Hkv, S, sinks)) return fail(CATTN_ERR_UNSUPPORTED, "grid too large, or too many sinks");
   if (!q || !k || !v || !o || !dout || !lse || !dq || !dk || !dv || !workspace)
     return fail(CATTN_ERR_INVALID_ARG, "NULL tensor pointer");
   if (!aligned(lse, 4) || !aligned(lens, 4)) return fail(CATTN_ERR_INVALID_ARG, "lse and lens must be 4-byte aligned");
@@ -447,7 +455,8 @@ cattn_status cattn_swa_bwd(const void* q, const void* k, const void* v, const vo
 
 size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, int window, int sinks, int dtype) {
   if (!valid_dtype(dtype)) return 0;
-  if (B <= 0 || Hq <= 0 || Hkv <= 0 || cap <= 0 || D <= 0 || window < 1 || sinks < 0 || Hq % Hkv) return 0;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || cap <= 0 || !swa_D(D) || window < 1 || sinks < 0 || Hq % Hkv) return 0;
+  if (!swa_fits(B, Hq, cap)) return 0;
   return sizeof(float) *
          (size_t)swa_decode_floats(dtype == CATTN_BF16, B, Hq, Hkv, cap, D, std::min(window, cap),
                                    std::min(sinks, cap));

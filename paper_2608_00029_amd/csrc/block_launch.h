@@ -11,6 +11,7 @@ namespace cattn {
 // ---------------------------------------------------------------------------
 // RMSNorm
 // ---------------------------------------------------------------------------
+constexpr int kRmsMaxRows = 1 << 30;
 constexpr int kRmsMaxC = 16384;  // widest row kept in registers (16 waves, 2 x 8 columns a lane)
 
 struct RmsFwd {
