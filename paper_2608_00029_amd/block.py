@@ -17,8 +17,8 @@ from typing import Optional
 
 import torch
 
-from .binding import (CATTN_BF16, CATTN_F32, CATTN_OK, CattnError, _check_workspace, _dtype_code, _LAYOUTS, _rows_cols,
-                      _stream, last_error_string, lib)
+from .binding import (CATTN_BF16, CATTN_ERR_UNSUPPORTED, CATTN_F32, CATTN_OK, CattnError, _check_workspace, _dtype_code,
+                      _LAYOUTS, _rows_cols, _stream, last_error_string, lib)
 
 _F32, _F64, _I32 = torch.float32, torch.float64, torch.int32
 _SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
@@ -90,8 +90,14 @@ def _at(t) -> int:
 
 
 def _int(n) -> int:
-    """n as a C int: what does not fit becomes the largest (or -1), which the library clamps or refuses."""
+    """n as a C int: what does not fit becomes the largest (or -1), which the library clamps or refuses.
+    (ctypes would hand over its low 32 bits.)"""
     return n if -1 <= n <= 2147483647 else 2147483647 if n > 0 else -1
+
+
+# Sizes (not negative) are all C ints iff none has a bit from 31 on: `(B | S | ...) >> 31` asks once for all.
+def _too_large(where):
+    raise CattnError(CATTN_ERR_UNSUPPORTED, where, "a size exceeds 2^31 - 1")
 
 
 def _heads(name, t, layout):
@@ -143,9 +149,11 @@ def _batch(name, t, B, device):
 # RMSNorm
 # ---------------------------------------------------------------------------
 # (empty_like costs less host time than new_empty, and that less than torch.empty with its keywords)
-def _norm_inputs(x, gamma, residual):
+def _norm_inputs(where, x, gamma, residual):
     _on_hip("x", x)
     R, C = _rows_cols(x)
+    if (R | C) >> 31:
+        _too_large(where)
     if not x.is_contiguous():
         raise ValueError("x must be contiguous")
     _plain("gamma", gamma, (C,), _F32, x.device)
@@ -161,10 +169,9 @@ def rmsnorm_fwd(x, gamma, residual=None, eps: float = 1e-5):
     x (and residual): float32 or bfloat16, contiguous; gamma: float32 [C].  h is
     x itself without a residual; rstd is float32 [rows].
     """
-    R, C, h, rstd, code = _norm_inputs(x, gamma, residual)
+    R, C, h, rstd, code = _norm_inputs("cattn_rmsnorm_fwd", x, gamma, residual)
     y = torch.empty_like(x)
-    _run("cattn_rmsnorm_fwd", x.device, _at(x), _at(residual), _at(gamma), _at(y), _at(h), _at(rstd), _int(R), C, eps,
-         code)
+    _run("cattn_rmsnorm_fwd", x.device, _at(x), _at(residual), _at(gamma), _at(y), _at(h), _at(rstd), R, C, eps, code)
     return y, x if h is None else h, rstd
 
 
@@ -174,19 +181,19 @@ def rmsnorm_fwd_q8(x, gamma, residual=None, eps: float = 1e-5, group: int = 0):
     q is float8_e4m3fn of x's shape; scale float32 [rows, ceil(C / group)], one per
     `group` consecutive columns (a power of two from 8 to 512), or one per row for 0.
     """
-    R, C, h, rstd, code = _norm_inputs(x, gamma, residual)
+    R, C, h, rstd, code = _norm_inputs("cattn_rmsnorm_fwd_q8", x, gamma, residual)
     if not isinstance(group, int) or (group and (group < 8 or group > 512 or group & (group - 1))):
         raise ValueError("group must be 0 or a power of two from 8 to 512")
     q = torch.empty_like(x, dtype=torch.float8_e4m3fn)
     scale = gamma.new_empty((R, -(-C // group) if group else 1))
     _run("cattn_rmsnorm_fwd_q8", x.device, _at(x), _at(residual), _at(gamma), _at(q), _at(scale), _at(h), _at(rstd),
-         _int(R), C, group, eps, code)
+         R, C, group, eps, code)
     return q, scale, x if h is None else h, rstd
 
 
 @functools.lru_cache(maxsize=256)  # (a call into the library each time costs 1 us)
 def rmsnorm_bwd_workspace_bytes(rows: int, C: int) -> int:
-    return int(lib().cattn_rmsnorm_bwd_workspace_bytes(rows, C))
+    return int(lib().cattn_rmsnorm_bwd_workspace_bytes(_int(rows), _int(C)))
 
 
 def rmsnorm_bwd(h, gamma, rstd, dy, dh=None, workspace=None):
@@ -197,6 +204,8 @@ def rmsnorm_bwd(h, gamma, rstd, dy, dh=None, workspace=None):
     """
     _on_hip("h", h)
     R, C = _rows_cols(h)
+    if (R | C) >> 31:
+        _too_large("cattn_rmsnorm_bwd")
     code = _dtype_code(h)
     if not h.is_contiguous():
         raise ValueError("h must be contiguous")
@@ -213,7 +222,7 @@ def rmsnorm_bwd(h, gamma, rstd, dy, dh=None, workspace=None):
     else:
         _check_workspace(workspace, n, h.device)
     _run("cattn_rmsnorm_bwd", h.device, _at(h), _at(gamma), _at(rstd), _at(dy), _at(dh), _at(dx), _at(dgamma),
-         _at(workspace), _int(R), C, code)
+         _at(workspace), R, C, code)
     return dx, dgamma
 
 
@@ -252,6 +261,9 @@ def _rope(q, k, freqs, positions, layout, interleaved, amplitude, q_out, k_out, 
     if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1:
         raise TypeError("freqs must be a 1-d float64 tensor (rope_frequencies)")
     _plain("freqs", freqs, freqs.shape, _F64, dev)
+    rot = 2 * freqs.shape[0]
+    if (B | Hq | Hkv | S | D | rot) >> 31:
+        _too_large("cattn_rope")
     batched = 0
     if positions is not None:
         batched = int(isinstance(positions, torch.Tensor) and positions.dim() == 2)
@@ -266,8 +278,8 @@ def _rope(q, k, freqs, positions, layout, interleaved, amplitude, q_out, k_out, 
         else:
             _view("k_out", k_out, k.shape, q.dtype, dev)
     strides = _strides((q, k, q_out, k_out) if k is not None else (q, q, q_out, q_out), layout)
-    _run("cattn_rope", dev, _at(q), _at(k), _at(q_out), _at(k_out), _at(positions), _at(freqs), _int(B), _int(S), Hq,
-         Hkv, D, 2 * freqs.shape[0], batched, strides, _LAYOUTS[layout], bool(interleaved), inverse, amplitude, code)
+    _run("cattn_rope", dev, _at(q), _at(k), _at(q_out), _at(k_out), _at(positions), _at(freqs), B, S, Hq, Hkv, D, rot,
+         batched, strides, _LAYOUTS[layout], bool(interleaved), inverse, amplitude, code)
     return q_out, k_out
 
 
@@ -314,6 +326,9 @@ def rope_append(q, k, v, k_cache, v_cache, lens, freqs, counts=None, window: int
     if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1:
         raise TypeError("freqs must be a 1-d float64 tensor (rope_frequencies)")
     _plain("freqs", freqs, freqs.shape, _F64, dev)
+    rot = 2 * freqs.shape[0]
+    if (B | Hq | Hkv | S | D | rot | cap) >> 31:
+        _too_large("cattn_rope_append")
     if q_out is None:
         q_out = _like(q)
     else:
@@ -324,8 +339,8 @@ def rope_append(q, k, v, k_cache, v_cache, lens, freqs, counts=None, window: int
         _view("k_out", k_out, k.shape, dt, dev)
     strides = _strides((q, k, v, q_out, k_out, k_cache, v_cache), layout)
     _run("cattn_rope_append", dev, _at(q), _at(k), _at(v), _at(q_out), _at(k_out), _at(k_cache), _at(v_cache),
-         _at(lens), _at(counts), _at(freqs), _int(B), _int(S), Hq, Hkv, D, 2 * freqs.shape[0], _int(cap), _int(window),
-         _int(sinks), bool(rolling), strides, _LAYOUTS[layout], bool(interleaved), amplitude, code)
+         _at(lens), _at(counts), _at(freqs), B, S, Hq, Hkv, D, rot, cap, _int(window), _int(sinks),
+         bool(rolling), strides, _LAYOUTS[layout], bool(interleaved), amplitude, code)
     return q_out, k_out
 
 
@@ -348,6 +363,8 @@ def swa_fwd(q, k, v, scale: float, window: int, sinks: int = 0, lens=None, layou
     _view("k", k, _shape(B, Hkv, S, D, layout), dt, dev)
     _view("v", v, k.shape, dt, dev)
     _batch("lens", lens, B, dev)
+    if (B | Hq | Hkv | S | D) >> 31:
+        _too_large("cattn_swa_fwd")
     if o is None:
         o = _like(q)
     else:
@@ -356,14 +373,14 @@ def swa_fwd(q, k, v, scale: float, window: int, sinks: int = 0, lens=None, layou
         lse = q.new_empty((B, Hq, S), dtype=_F32)
     else:
         _plain("lse", lse, (B, Hq, S), _F32, dev)
-    _run("cattn_swa_fwd", dev, _at(q), _at(k), _at(v), _at(o), _at(lse), _at(lens), B, Hq, Hkv, _int(S), D,
-         _int(window), _int(sinks), scale, _strides((q, k, v, o), layout), _LAYOUTS[layout], code)
+    _run("cattn_swa_fwd", dev, _at(q), _at(k), _at(v), _at(o), _at(lse), _at(lens), B, Hq, Hkv, S, D, _int(window),
+         _int(sinks), scale, _strides((q, k, v, o), layout), _LAYOUTS[layout], code)
     return o, lse
 
 
 @functools.lru_cache(maxsize=256)
 def swa_bwd_workspace_bytes(B: int, Hq: int, Hkv: int, S: int, D: int, window: int, sinks: int = 0) -> int:
-    return int(lib().cattn_swa_bwd_workspace_bytes(B, Hq, Hkv, S, D, _int(window), _int(sinks)))
+    return int(lib().cattn_swa_bwd_workspace_bytes(*map(_int, (B, Hq, Hkv, S, D, window, sinks))))
 
 
 def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens=None, layout: str = "bhsd",
@@ -379,6 +396,8 @@ def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens
         _view(n, t, shape, dt, dev)
     _plain("lse", lse, (B, Hq, S), _F32, dev)
     _batch("lens", lens, B, dev)
+    if (B | Hq | Hkv | S | D) >> 31:
+        _too_large("cattn_swa_bwd")
     for n, t, shape in (("dq", dq, q.shape), ("dk", dk, kv), ("dv", dv, kv)):
         if t is not None:
             _view(n, t, shape, dt, dev)
@@ -391,7 +410,7 @@ def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens
     else:
         _check_workspace(workspace, n, dev)
     _run("cattn_swa_bwd", dev, _at(q), _at(k), _at(v), _at(o), _at(do), _at(lse), _at(lens), _at(dq), _at(dk), _at(dv),
-         _at(workspace), B, Hq, Hkv, _int(S), D, _int(window), _int(sinks), scale,
+         _at(workspace), B, Hq, Hkv, S, D, _int(window), _int(sinks), scale,
          _strides((q, k, v, o, do, dq, dk, dv), layout), _LAYOUTS[layout], code)
     return dq, dk, dv
 
@@ -400,7 +419,7 @@ def swa_bwd(q, k, v, o, do, lse, scale: float, window: int, sinks: int = 0, lens
 def swa_decode_workspace_bytes(B: int, Hq: int, Hkv: int, cap: int, D: int, window: int, sinks: int = 0,
                                dtype: Optional[torch.dtype] = None) -> int:
     """Bytes of swa_decode's workspace; without a dtype what either takes."""
-    sizes = (B, Hq, Hkv, cap, D, _int(window), _int(sinks))
+    sizes = tuple(map(_int, (B, Hq, Hkv, cap, D, window, sinks)))
     codes = {torch.float32: (CATTN_F32,), torch.bfloat16: (CATTN_BF16,)}.get(dtype, (CATTN_F32, CATTN_BF16))
     return max(int(lib().cattn_swa_decode_workspace_bytes(*sizes, code)) for code in codes)
 
@@ -425,6 +444,8 @@ def swa_decode(q, k_cache, v_cache, lens, scale: float, window: int, sinks: int 
     _view("k_cache", k_cache, _shape(B, Hkv, cap, D, layout), dt, dev)
     _view("v_cache", v_cache, k_cache.shape, dt, dev)
     _plain("lens", lens, (B,), _I32, dev)
+    if (B | Hq | Hkv | cap | D) >> 31:
+        _too_large("cattn_swa_decode")
     if o is None:
         o = _like(q)
     else:
@@ -439,6 +460,6 @@ def swa_decode(q, k_cache, v_cache, lens, scale: float, window: int, sinks: int 
     else:
         _check_workspace(workspace, n, dev)
     _run("cattn_swa_decode", dev, _at(q), _at(k_cache), _at(v_cache), _at(o), _at(lse), _at(lens), _at(workspace), B,
-         Hq, Hkv, _int(cap), D, _int(window), _int(sinks), bool(rolling), scale,
+         Hq, Hkv, cap, D, _int(window), _int(sinks), bool(rolling), scale,
          _strides((q, k_cache, v_cache, o), layout), _LAYOUTS[layout], code)
     return o, lse
