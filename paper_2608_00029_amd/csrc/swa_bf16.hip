@@ -759,40 +759,6 @@ template <int ROWS> dim3 rows_grid(const SwaArgs& a, int heads) {
   return dim3((unsigned)((int64_t)a.B * heads * ((a.S + ROWS - 1) / ROWS)));
 }
 
-// How a kernel's work groups divide their walk over the other axis: not (128 rows
-// of four waves), in two parts (64 rows) or in four (32 rows).  A grid of few
-// 128-row work groups leaves CUs idle and its waves the whole walk; more parts cost
-// rings, LDS and the parts' merge.  What decides are the 32-row groups per CU, g, and
-// `run`, the tiles a work group walks (of all heads of the group in dK/dV).
-// Measured, none / two / four parts, us (MHA unless Hq/Hkv; F forward, Q dQ, K dK/dV
-// with the other kernel's time in; S, window):
-//   D  64  g 1    F 15.5 / 10.5 / 9.0 (1024, 512), K 180 / 144 / 123 (8192, 4096)
-//          g 2    F 9.7 / 8.7 / 8.8, K 23.0 / 20.2 / 20.7 (1024, 128); F 15.5 / 10.7 / 9.9, K 38.3 / 32.2 / 30.7
-//                 (1024, 512); K 8/2 267 / 188 / 176 (8192, 2048)
-//          g 4    F 15.9 / 12.8 / 16.7, K 39.1 / 36.0 / 40.8 (1024, 512); K 16/4 183 / 161 / 185 (8192, 1024)
-//          g 6    F 12.0 / 13.6, K 30.5 / 32.5 (1024, 128); F 69.1 / 71.8, K 190 / 199 (8192, 4096)
-//   D 128  g 1    F 22.0 / 13.5 / 11.4, K 55.7 / 45.1 / 40.7 (1024, 512)
-//          g 2    F 14.0 / 9.6 / 15.3, K 33.2 / 28.3 / 35.6 (1024, 128); K 8/2 424 / 288 / 341 (8192, 2048)
-//          g 3    Q 53.3 / 56.1, K 54.5 / 49.4 (1152, 40/20, 130); Q 71.2 / 64.8, K 70.0 / 59.2 (1024, 1024);
-//                 Q 370 / 365, K 458 / 365 (6144, 16/4, 2048)
-//          g 4    F 14.8 / 12.2, Q 36.3 / 37.3, K 35.8 / 35.6 (1024, 128); F 22.6 / 17.4, Q 55.3 / 54.5, K 55.6 / 51.8
-//                 (1024, 512); Q 252 / 264, K 281 / 253 (8192, 16/4, 1024)
-//          g 5    F 15.5 / 17.6 (5000, 8), 21.4 / 22.0 (5000, 200), 29.6 / 27.8 (5000, 512), 57.6 / 49.8 (5000, 2048);
-//                 K 76.8 / 79.7 (5000, 512)
-//          g 6    F 19.9 / 19.3 (1024, 128), 109 / 117 (8192, 4096); Q 319 / 341, K 321 / 364 (8192, 4096)
-enum Form { kWhole = 1, kTwo = 2, kFour = 4 };
-Form form_of(Pass pass, int D, int64_t heads, int S, int run) {
-  const int64_t groups = heads * ((S + 31) / 32), cus = cu_count();
-  if (groups <= cus || (D == 64 && groups <= 2 * cus && run >= 16)) return kFour;
-  if (groups > (D == 128 && pass == Pass::kFwd && run >= 16 ? 5 : 4) * cus) return kWhole;
-  if (D == 128 && pass == Pass::kDq && groups > 2 * cus && run < 16) return kWhole;
-  return kTwo;
-}
-// Tiles that a work group of 128 rows walks on one head.
-int run_of(const SwaArgs& a) {
-  return std::min((a.S + 31) / 32, (std::min(a.window, a.S) + 127) / 32 + swa_sink_tiles(a.S, a.sinks));
-}
-
 template <int D, int SPLIT, int NB> hipError_t fwd_s(const SwaArgs& a, float c, hipStream_t st) {
   hipLaunchKernelGGL((swa_fwd_bf16_kernel<D, SPLIT, NB>), rows_grid<128 / SPLIT>(a, a.Hq), dim3(256), 0, st, a, c);
   return hipGetLastError();
@@ -809,28 +775,25 @@ template <int D, int SPLIT, int NB> hipError_t dkdv_s(const SwaArgs& a, float c,
 
 template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
-  switch (form_of(Pass::kFwd, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
+  const int run = swa_run(a.S, a.window, a.sinks);
+  switch (swa_form(Pass::kFwd, D, (int64_t)a.B * a.Hq, a.S, run)) {
     case kFour: return fwd_s<D, 4, 2>(a, c, st);
     case kTwo: return fwd_s<D, 2, D == 64 ? 4 : 2>(a, c, st);
     default: break;
   }
-  // A ring of four (a barrier every second tile) holds two work groups of D = 128 a
-  // CU, one of three holds three: better from the third on (four / three, us: B4 H12
-  // S1024 window 256, 384 work groups, 22.6 / 24.3; B1 H16 S4096 window 4096, 512, 99.8
-  // / 102.8; B1 H12 S8192 window 1024, 768, 77.9 / 73.1).
-  const bool two = (int64_t)a.B * a.Hq * ((a.S + 127) / 128) <= 2 * (int64_t)cu_count();
-  return D == 64 || two ? fwd_s<D, 1, 4>(a, c, st) : fwd_s<D, 1, 3>(a, c, st);
+  return swa_fwd_ring(D, (int64_t)a.B * a.Hq, a.S) == 4 ? fwd_s<D, 1, 4>(a, c, st) : fwd_s<D, 1, 3>(a, c, st);
 }
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
+  const int run = swa_run(a.S, a.window, a.sinks);
   hipError_t e;
-  switch (form_of(Pass::kDq, D, (int64_t)a.B * a.Hq, a.S, run_of(a))) {
+  switch (swa_form(Pass::kDq, D, (int64_t)a.B * a.Hq, a.S, run)) {
     case kFour: e = dq_s<D, 4, 2>(a, c, st); break;
     case kTwo: e = dq_s<D, 2, D == 64 ? 4 : 2>(a, c, st); break;
     default: e = dq_s<D, 1, 4>(a, c, st);
   }
   if (e != hipSuccess) return e;
-  const Form form = form_of(Pass::kDkdv, D, (int64_t)a.B * a.Hkv, a.S, run_of(a) * (a.Hq / a.Hkv));
+  const SwaForm form = swa_form(Pass::kDkdv, D, (int64_t)a.B * a.Hkv, a.S, run * (a.Hq / a.Hkv));
   const bool shared = form == kFour && swa_far_shares(true, a.B, a.Hq, a.Hkv, a.S, a.D, a.window, a.sinks);
   const int far = swa_far_parts(true, shared, a.B, a.Hq, a.Hkv, a.S, a.window, a.sinks);
   const int n_far = a.B * a.Hkv * swa_sink_tiles(a.S, a.sinks) * far;
