@@ -781,7 +781,10 @@ template <int D> hipError_t fwd_d(const SwaArgs& a, hipStream_t st) {
     case kTwo: return fwd_s<D, 2, D == 64 ? 4 : 2>(a, c, st);
     default: break;
   }
-  return swa_fwd_ring(D, (int64_t)a.B * a.Hq, a.S) == 4 ? fwd_s<D, 1, 4>(a, c, st) : fwd_s<D, 1, 3>(a, c, st);
+  if constexpr (D == 128) {  // (the ring of three is only built where the rule can ask for it)
+    if (swa_fwd_ring(D, (int64_t)a.B * a.Hq, a.S) == 3) return fwd_s<D, 1, 3>(a, c, st);
+  }
+  return fwd_s<D, 1, 4>(a, c, st);
 }
 template <int D> hipError_t bwd_d(const SwaArgs& a, hipStream_t st) {
   const float c = a.scale * kLog2e;
