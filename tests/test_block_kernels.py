@@ -36,3 +36,8 @@ def test_no_form_without_a_call(kernels):
     """The forward's ring of three is D = 128's: the rule takes four slots at D = 64 on every grid."""
     rings = {(int(m[1]), int(m[2]), int(m[3])) for m in (re.search(r"swa_fwd_bf16_kernelILi(\d+)ELi(\d)ELi(\d)E", n) for n in kernels) if m}
     assert rings == {(64, 1, 4), (64, 2, 4), (64, 4, 2), (128, 1, 4), (128, 1, 3), (128, 2, 2), (128, 4, 2)}
+
+
+def test_no_kernel_spills(kernels):
+    """All operands of a row or a tile stay in vector registers: nothing goes through scratch memory."""
+    assert {n: k for n, k in kernels.items() if k != (0, 0)} == {}
