@@ -240,6 +240,8 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", fac
     if scaling not in _SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(_SCALINGS)}, not {scaling!r}")
     rot = int(rot)
+    if rot > 2147483647:
+        _too_large("cattn_rope_frequencies")
     out = (ctypes.c_double * max(1, rot // 2))()
     st = lib().cattn_rope_frequencies(out, rot, base, _SCALINGS[scaling], factor, context, low, high)
     if st != CATTN_OK:

@@ -86,6 +86,14 @@ def test_the_calls_are_otherwise_taken(host):
             call()
 
 
+def test_frequencies_of_a_size_beyond_an_int(monkeypatch):
+    """Refused before anything of that size is allocated."""
+    monkeypatch.setattr(block.ctypes, "c_double", None)
+    for rot in (1 << 31, WRAP + 64):
+        with pytest.raises(cattn.CattnError, match="2\\^31"):
+            cattn.rope_frequencies(rot)
+
+
 def test_workspaces_of_refused_sizes():
     """None, and no overflow on the way."""
     big = (1 << 31) - 1
