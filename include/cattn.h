@@ -431,7 +431,9 @@ cattn_status cattn_rope_append(const void* q, const void* k, const void* v, void
  *     j <= i  and  (i - j < window  or  j < sinks)
  * (window counts the query itself; window >= S is plain causal attention).
  * Forward and backward compute cattn_attn_fwd's and cattn_attn_bwd's formulas
- * over those pairs; dK and dV sum over the query heads of a group.
+ * over those pairs; dK and dV sum over the query heads of a group.  Hidden pairs
+ * are left out, not scored with the sentinel, but it is where a row's running
+ * maximum begins: products q . k are to lie above -1e30.
  *
  *   q, o, dout, dq: [B, Hq, S, D]; k, v, dk, dv: [B, Hkv, S, D] `dtype`, in
  *             `layout`'s order or strided (order: q, k, v, o of the forward; q,

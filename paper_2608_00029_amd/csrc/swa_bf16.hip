@@ -15,10 +15,13 @@
 //  * Grouped heads: query heads read their group's key/value head; a dK/dV
 //    work group walks the query tiles of all heads of its group, which sums
 //    the group's gradients in float32 in a fixed order.
-//  * Sinks in dK/dV: a sink's queries reach to the end of the sequence.  The
-//    window's work groups leave out the pairs that only the sinks see, others
-//    take those in parts (swa_far_parts), and another kernel sums the partial
-//    results in order: no work group runs longer than the others.
+//  * Sinks in dK/dV: a sink's queries reach to the end of the sequence.  Where they
+//    are few, the work groups that own the sinks walk them too (swa_has_far: up to
+//    512 a group, 16 tiles).  Else the window's work groups leave out the pairs that
+//    only the sinks see, others take those in parts (swa_far_parts), and another
+//    kernel sums the partial results in order.  Parts go as far as to give each CU a
+//    work group: with 256 tiles of sinks and more over all heads, each far work
+//    group still walks to its sequence's end.
 //  * Padded batches: rows from lens[b] on are never read (a tile that reaches
 //    past the end repeats the last row, masked), so they may hold anything;
 //    their O and gradients are 0 and their LSE -inf.

@@ -17,8 +17,9 @@ constexpr int64_t kSwaCus = 256;  // compute units of the one GPU these kernels 
 // Where those far queries of all heads of a group are many, the window's work
 // groups leave them out, and others take them: the far (query head, 32-query tile)
 // pairs of a 32-key tile of sinks cut into parts, so that the parts of all heads
-// give the GPU one work group per CU (what its LDS holds at D = 128), but a part has
-// at least a tile for each of its waves.  Each part leaves float32 partial sums.
+// give the GPU one work group per CU (what its LDS holds at D = 128), but at most one
+// part for every four tiles, a tile per wave.  From 256 tiles of sinks on, over
+// all heads, a part is the whole walk.  Each part leaves float32 partial sums.
 // Backward, 4 sinks, us, with a grid of their own / without, by far queries times
 // heads of the group:
 //   bf16  256: B1 H4 S1024 D64 35.6 / 27.0;  384: B4 H8 S512 D128 39.6 / 34.5;
@@ -61,8 +62,10 @@ constexpr int64_t swa_far_floats(int B, int Hq, int Hkv, int S, int D, int windo
 }
 
 // Decoding: parts that the visible slots of one (sequence, key/value head, 32 query
-// heads) are cut into, each a work group of four waves that stream 32-slot tiles;
-// one of several parts has at least four tiles, one per wave.  Parts cost a second
+// heads) are cut into, each a work group of four waves that stream 32-slot tiles; at
+// most one part for every four tiles that can be seen, a tile per wave, or fewer in
+// the last (513 slots are 17 tiles, in five parts 4, 4, 4, 4 and 1) and in those of
+// a sequence that has not filled its cache.  Parts cost a second
 // kernel, 4 us, that joins them, so there is one where the slots are few; else as
 // many as give each CU at most one work group (one more is a second round).  In
 // bf16 two or three do not pay: 86 work groups take most of the bandwidth.  In
