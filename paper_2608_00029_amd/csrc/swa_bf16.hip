@@ -20,8 +20,8 @@
 //    512 a group, 16 tiles).  Else the window's work groups leave out the pairs that
 //    only the sinks see, others take those in parts (swa_far_parts), and another
 //    kernel sums the partial results in order.  Parts go as far as to give each CU a
-//    work group: with 256 tiles of sinks and more over all heads, each far work
-//    group still walks to its sequence's end.
+//    work group: with over 128 tiles of sinks in all heads each far work group
+//    still walks to its sequence's end.
 //  * Padded batches: rows from lens[b] on are never read (a tile that reaches
 //    past the end repeats the last row, masked), so they may hold anything;
 //    their O and gradients are 0 and their LSE -inf.

@@ -18,8 +18,8 @@ constexpr int64_t kSwaCus = 256;  // compute units of the one GPU these kernels 
 // groups leave them out, and others take them: the far (query head, 32-query tile)
 // pairs of a 32-key tile of sinks cut into parts, so that the parts of all heads
 // give the GPU one work group per CU (what its LDS holds at D = 128), but at most one
-// part for every four tiles, a tile per wave.  From 256 tiles of sinks on, over
-// all heads, a part is the whole walk.  Each part leaves float32 partial sums.
+// part for every four tiles, a tile per wave.  With over 128 tiles of sinks in
+// all heads a part is the whole walk.  Each part leaves float32 partial sums.
 // Backward, 4 sinks, us, with a grid of their own / without, by far queries times
 // heads of the group:
 //   bf16  256: B1 H4 S1024 D64 35.6 / 27.0;  384: B4 H8 S512 D128 39.6 / 34.5;
