@@ -1,0 +1,253 @@
+"""The operators of a decoder block's feed-forward half: the gated projections
+(both products, the activation and their product, with the backward pass; and
+for the few rows of single tokens), and dropout with the residual added, whose
+mask comes from a counter-based generator and is never stored.  Each case is one
+call, or a forward and its backward, as a program makes it.
+
+listed() names twelve cases; draw() takes others of the same ranges; prepare()
+makes what a program has in hand; run() is one pass: with `own` false in plain
+torch arithmetic (32-bit, random words in integers), with `own` true through the
+package; exact() gives the same outputs in 64 bits; work() the bytes and
+operations a pass cannot do without.
+"""
+
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+WORD = 0xFFFFFFFF
+
+
+def _gated(name, T, C, F, dtype="bf16", activation="silu", backward=False):
+    return {"name": name, "op": "gated", "T": T, "C": C, "F": F, "dtype": dtype, "activation": activation,
+            "backward": backward}
+
+
+def _dropout(name, rows, C, dtype="bf16", residual=True, p=0.1, backward=False, step=0):
+    return {"name": name, "op": "dropout", "rows": rows, "C": C, "dtype": dtype, "residual": residual, "p": p,
+            "backward": backward, "step": step}
+
+
+def listed():
+    return [
+        # The feed-forward block of GPT-2 XL's width in training, 8 sequences of 1024 tokens, mixed precision.
+        _gated("gated_train", 8192, 1600, 4288, backward=True),
+        # The same at GPT-2 medium's width and tanh GELU, a batch whose tokens, packed without padding, fill no tile.
+        _gated("gated_train_odd", 3777, 1024, 2728, activation="gelu", backward=True),
+        # Full precision, GPT-2 small's width.
+        _gated("gated_train_f32", 2048, 768, 2048, dtype="f32", backward=True),
+        # A prompt batch of a wide model.
+        _gated("gated_prompt", 4096, 4096, 10240),
+        # One step of a server: new prompts' pieces beside single tokens.
+        _gated("gated_mixed", 200, 2048, 5632, activation="gelu"),
+        # One decoding step of 24 sequences of a wide model: the weights' bandwidth.
+        _gated("gated_tokens", 24, 4096, 10240),
+        # One sequence's next token at GPT-2 XL's width: latency.
+        _gated("gated_one", 1, 1600, 4288),
+        # The same in full precision.
+        _gated("gated_one_f32", 1, 768, 2048, dtype="f32", activation="gelu"),
+        # Dropout after a projection of GPT-2 XL, residual added; the backward reads the upstream gradient alone.
+        _dropout("dropout_train", 8192, 1600, backward=True),
+        # GPT-2 small's embeddings in full precision, no residual.
+        _dropout("dropout_embeddings_f32", 16384, 768, dtype="f32", residual=False, backward=True),
+        # A large micro-batch of a wide model, the step's counter in device memory as a captured graph needs it.
+        _dropout("dropout_wide", 16384, 4096, p=0.25, step=12345),
+        # One short sequence: latency.
+        _dropout("dropout_short", 33, 768),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
+    if rng.random() < 0.65:
+        backward = rng.random() < 0.5
+        C = max(64, _log_int(rng, 64, 5120) // 8 * 8)
+        F = max(64, int(C * rng.uniform(1.0, 4.0)) // 8 * 8)
+        if rng.random() < 0.5:
+            C, F = max(64, C // 64 * 64), max(64, F // 64 * 64)
+        room = 8192 * 1600 * 4288 // (1 if backward else 2) // (1 if dtype == "bf16" else 16)
+        T = _log_int(rng, 1, max(1, min(8192, room // (C * F))))
+        return _gated("", T, C, F, dtype, rng.choice(["silu", "gelu"]), backward)
+    C = max(8, _log_int(rng, 64, 8192) // 8 * 8)
+    backward = rng.random() < 0.5
+    rows = _log_int(rng, 1, min(16384, 16384 * 4096 // C // (2 if dtype == "f32" else 1) // (2 if backward else 1)))
+    return _dropout("", rows, C, dtype, rng.random() < 0.6, rng.choice([0.05, 0.1, 0.25, 0.5]), backward,
+                    rng.choice([0, 0, 1 << 40]))
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+
+    def randn(*shape):
+        return torch.randn(shape, generator=g, dtype=torch.float32, device="cuda")
+
+    if case["op"] == "gated":  # x as a norm leaves it, weights that keep its size
+        T, C, F = case["T"], case["C"], case["F"]
+        st = {"x": randn(T, C).to(dt), "w_gate": (randn(F, C) / math.sqrt(C)).to(dt),
+              "w_up": (randn(F, C) / math.sqrt(C)).to(dt)}
+        if case["backward"]:
+            st["dh"] = randn(T, F).to(dt)
+        return st | {"case": case}
+    R, C = case["rows"], case["C"]
+    st = {"x": randn(R, C).to(dt), "residual": (3.0 * randn(R, C)).to(dt) if case["residual"] else None,
+          "seed": (seed * 0x9E3779B97F4A7C15 + 0x1234567) & 0x7FFFFFFFFFFFFFFF, "stream": seed % 48,
+          "step": torch.tensor([case["step"]], dtype=torch.int64, device="cuda") if case["step"] else None}
+    if case["backward"]:
+        st["dy"] = randn(R, C).to(dt)
+    return st | {"case": case}
+
+
+# ---------------------------------------------------------------------------
+# The plain forms
+# ---------------------------------------------------------------------------
+def _plain_gated(s, case):
+    dt = s["x"].dtype
+    x, wg, wu = s["x"].float(), s["w_gate"].float(), s["w_up"].float()
+    gate, up = x @ wg.t(), x @ wu.t()
+    if case["activation"] == "silu":
+        sig = 1.0 / (1.0 + torch.exp(-gate))
+        act = gate * sig
+    else:
+        th = torch.tanh(math.sqrt(2.0 / math.pi) * (gate + 0.044715 * gate * gate * gate))
+        act = 0.5 * gate * (1.0 + th)
+    out = {"h": (act * up).to(dt)}
+    if not case["backward"]:
+        return out
+    if case["activation"] == "silu":
+        slope = sig * (1.0 + gate * (1.0 - sig))
+    else:
+        slope = 0.5 * (1.0 + th) + 0.5 * gate * (1.0 - th * th) * math.sqrt(2.0 / math.pi) * (
+            1.0 + 3 * 0.044715 * gate * gate)
+    dh = s["dh"].float()
+    dgate, dup = dh * up * slope, dh * act
+    return out | {"gate": gate.to(dt), "up": up.to(dt), "dx": (dgate @ wg + dup @ wu).to(dt),
+                  "dw_gate": (dgate.t() @ x).to(dt), "dw_up": (dup.t() @ x).to(dt)}
+
+
+def _words(n, seed, stream):
+    """The first n random words: Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers:
+    as easy as 1, 2, 3", 2011) of the counters (i, stream), four words each, under the key `seed`."""
+    i = torch.arange((n + 3) // 4, dtype=torch.int64, device="cuda")
+    c = [i & WORD, i >> 32, torch.full_like(i, stream & WORD), torch.full_like(i, stream >> 32 & WORD)]
+    k0, k1 = seed & WORD, seed >> 32 & WORD
+    for _ in range(10):
+        a, b = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57  # (mod 2^64; the low 64 bits are the product's)
+        c = [(b >> 32 & WORD) ^ c[1] ^ k0, b & WORD, (a >> 32 & WORD) ^ c[3] ^ k1, a & WORD]
+        k0, k1 = (k0 + 0x9E3779B9) & WORD, (k1 + 0xBB67AE85) & WORD
+    return torch.stack(c, 1).view(-1)[:n]
+
+
+def _plain_dropout(s, case):
+    x, p = s["x"], case["p"]
+    stream = s["stream"] + (int(case["step"]) if s["step"] is not None else 0)
+    keep = (_words(x.numel(), s["seed"], stream) >= round(p * 2.0 ** 32)).view(x.shape)
+    scale, zero = 1.0 / (1.0 - p), torch.zeros((), device=x.device)
+    y = torch.where(keep, x.float() * scale, zero)
+    out = {"y": (y + s["residual"].float() if case["residual"] else y).to(x.dtype)}
+    if case["backward"]:
+        out["dx"] = torch.where(keep, s["dy"].float() * scale, zero).to(x.dtype)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# The package's operators
+# ---------------------------------------------------------------------------
+def _own(s, case):
+    import paper_2608_00029_amd as cattn
+
+    if case["op"] == "gated":
+        x, wg, wu, act = s["x"], s["w_gate"], s["w_up"], case["activation"]
+        h, gate, up = cattn.gated_fwd(x, wg, wu, activation=act, save=case["backward"])
+        if not case["backward"]:
+            return {"h": h}
+        dx, dwg, dwu = cattn.gated_bwd(x, wg, wu, gate, up, s["dh"], activation=act)
+        return {"h": h, "gate": gate, "up": up, "dx": dx, "dw_gate": dwg, "dw_up": dwu}
+    how = {"stream": s["stream"], "step": s["step"]}
+    out = {"y": cattn.dropout_fwd(s["x"], case["p"], s["seed"], residual=s["residual"], **how)}
+    if case["backward"]:
+        out["dx"] = cattn.dropout_bwd(s["dy"], case["p"], s["seed"], **how)
+    return out
+
+
+def run(s):
+    case = s["case"]
+    if own:
+        return _own(s, case)
+    return _plain_gated(s, case) if case["op"] == "gated" else _plain_dropout(s, case)
+
+
+# ---------------------------------------------------------------------------
+# 64 bits
+# ---------------------------------------------------------------------------
+def _exact_gated(s, case):
+    x, wg, wu = (s[n].double() for n in ("x", "w_gate", "w_up"))
+    gate, up = x @ wg.t().contiguous(), x @ wu.t().contiguous()
+    gate.requires_grad_(case["backward"])
+    up.requires_grad_(case["backward"])
+    # both activations through one sigmoid: x sigmoid(x), and tanh(u) = 2 sigmoid(2 u) - 1
+    z = gate if case["activation"] == "silu" else 2 * math.sqrt(2 / math.pi) * (gate + 0.044715 * gate.pow(3))
+    h = gate * torch.sigmoid(z) * up
+    out = {"h": h.detach()}
+    if not case["backward"]:
+        return out
+    dg, du = torch.autograd.grad(h, (gate, up), s["dh"].double())
+    return out | {"gate": gate.detach(), "up": up.detach(), "dx": dg @ wg + du @ wu,
+                  "dw_gate": dg.t().contiguous() @ x, "dw_up": du.t().contiguous() @ x}
+
+
+def _mulhilo(m, v):
+    """(high, low) 32 bits of m v, from 16-bit parts."""
+    lo, hi = m & 0xFFFF, m >> 16
+    v0, v1 = v & 0xFFFF, v >> 16
+    mid = lo * v1 + (lo * v0 >> 16)
+    low_mid = hi * v0 + (mid & 0xFFFF)
+    return hi * v1 + (mid >> 16) + (low_mid >> 16), ((low_mid & 0xFFFF) << 16) | (lo * v0 & 0xFFFF)
+
+
+def _exact_dropout(s, case):
+    x, p = s["x"], case["p"]
+    n, seed = x.numel(), s["seed"]
+    stream = s["stream"] + case["step"]
+    kept = torch.empty((n + 3) // 4 * 4, dtype=torch.bool, device="cuda")
+    for at in range(0, (n + 3) // 4, 1 << 22):
+        i = torch.arange(at, min(at + (1 << 22), (n + 3) // 4), device="cuda")
+        x0, x1, x2, x3 = i % 2 ** 32, i // 2 ** 32, torch.full_like(i, stream % 2 ** 32), torch.full_like(i, stream // 2 ** 32)
+        for r in range(10):
+            key0, key1 = (seed + r * 0x9E3779B9) % 2 ** 32, (seed // 2 ** 32 + r * 0xBB67AE85) % 2 ** 32
+            h0, l0 = _mulhilo(0xD2511F53, x0)
+            h1, l1 = _mulhilo(0xCD9E8D57, x2)
+            x0, x1, x2, x3 = h1 ^ x1 ^ key0, l1, h0 ^ x3 ^ key1, l0
+        for e, word in enumerate((x0, x1, x2, x3)):
+            kept[4 * at + e:4 * (at + i.numel()):4] = word >= round(p * 2.0 ** 32)
+    mask = kept[:n].view(x.shape).double() / (1 - p)
+    y = x.double() * mask
+    out = {"y": y + s["residual"].double() if case["residual"] else y}
+    return out | ({"dx": s["dy"].double() * mask} if case["backward"] else {})
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return _exact_gated(s, case) if case["op"] == "gated" else _exact_dropout(s, case)
+
+
+def work(case):
+    e = 2 if case["dtype"] == "bf16" else 4
+    if case["op"] == "gated":
+        T, C, F = case["T"], case["C"], case["F"]
+        elements, flops = T * C + 2 * F * C + T * F, 4 * T * C * F + 8 * T * F
+        if case["backward"]:  # the saved products out and in, x and the weights again, the gradients
+            elements += 4 * T * F + T * C + 2 * F * C + T * F + T * C + 2 * F * C
+            flops += 8 * T * C * F + 16 * T * F
+        return {"bytes": elements * e, "flops": flops}
+    n = case["rows"] * case["C"]
+    passes = (3 if case["residual"] else 2) + (2 if case["backward"] else 0)
+    return {"bytes": passes * n * e, "flops": (2 + 2 * case["backward"]) * n}
