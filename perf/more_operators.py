@@ -99,8 +99,8 @@ def prepare(case, seed):
         return st | {"case": case}
     R, C = case["rows"], case["C"]
     st = {"x": randn(R, C).to(dt), "residual": (3.0 * randn(R, C)).to(dt) if case["residual"] else None,
-          "seed": (seed * 0x9E3779B97F4A7C15 + 0x1234567) & 0x7FFFFFFFFFFFFFFF, "stream": seed % 48,
-          "step": torch.tensor([case["step"]], dtype=torch.int64, device="cuda") if case["step"] else None}
+          "seed": (seed * 0x9E3779B97F4A7C15 + 0x1234567) & 0xFFFFFFFFFFFFFFFF, "site": seed % 48,
+          "step": torch.tensor([case["step"]], dtype=torch.int64, device="cuda") if case["step"] else 0}
     if case["backward"]:
         st["dy"] = randn(R, C).to(dt)
     return st | {"case": case}
@@ -133,11 +133,11 @@ def _plain_gated(s, case):
                   "dw_gate": (dgate.t() @ x).to(dt), "dw_up": (dup.t() @ x).to(dt)}
 
 
-def _words(n, seed, stream):
+def _words(n, seed, site, step):
     """The first n random words: Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers:
-    as easy as 1, 2, 3", 2011) of the counters (i, stream), four words each, under the key `seed`."""
+    as easy as 1, 2, 3", 2011) of the counters (i, site, step), four words each, under the key `seed`."""
     i = torch.arange((n + 3) // 4, dtype=torch.int64, device="cuda")
-    c = [i & WORD, i >> 32, torch.full_like(i, stream & WORD), torch.full_like(i, stream >> 32 & WORD)]
+    c = [i, torch.full_like(i, site), torch.full_like(i, step & WORD), torch.full_like(i, step >> 32)]
     k0, k1 = seed & WORD, seed >> 32 & WORD
     for _ in range(10):
         a, b = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57  # (mod 2^64; the low 64 bits are the product's)
@@ -148,8 +148,7 @@ def _words(n, seed, stream):
 
 def _plain_dropout(s, case):
     x, p = s["x"], case["p"]
-    stream = s["stream"] + (int(case["step"]) if s["step"] is not None else 0)
-    keep = (_words(x.numel(), s["seed"], stream) >= round(p * 2.0 ** 32)).view(x.shape)
+    keep = (_words(x.numel(), s["seed"], s["site"], case["step"]) >= round(p * 2.0 ** 32)).view(x.shape)
     scale, zero = 1.0 / (1.0 - p), torch.zeros((), device=x.device)
     y = torch.where(keep, x.float() * scale, zero)
     out = {"y": (y + s["residual"].float() if case["residual"] else y).to(x.dtype)}
@@ -171,7 +170,7 @@ def _own(s, case):
             return {"h": h}
         dx, dwg, dwu = cattn.gated_bwd(x, wg, wu, gate, up, s["dh"], activation=act)
         return {"h": h, "gate": gate, "up": up, "dx": dx, "dw_gate": dwg, "dw_up": dwu}
-    how = {"stream": s["stream"], "step": s["step"]}
+    how = {"site": s["site"], "step": s["step"]}
     out = {"y": cattn.dropout_fwd(s["x"], case["p"], s["seed"], residual=s["residual"], **how)}
     if case["backward"]:
         out["dx"] = cattn.dropout_bwd(s["dy"], case["p"], s["seed"], **how)
@@ -216,11 +215,11 @@ def _mulhilo(m, v):
 def _exact_dropout(s, case):
     x, p = s["x"], case["p"]
     n, seed = x.numel(), s["seed"]
-    stream = s["stream"] + case["step"]
+    step = case["step"]
     kept = torch.empty((n + 3) // 4 * 4, dtype=torch.bool, device="cuda")
     for at in range(0, (n + 3) // 4, 1 << 22):
         i = torch.arange(at, min(at + (1 << 22), (n + 3) // 4), device="cuda")
-        x0, x1, x2, x3 = i % 2 ** 32, i // 2 ** 32, torch.full_like(i, stream % 2 ** 32), torch.full_like(i, stream // 2 ** 32)
+        x0, x1, x2, x3 = i, torch.full_like(i, s["site"]), torch.full_like(i, step % 2 ** 32), torch.full_like(i, step // 2 ** 32)
         for r in range(10):
             key0, key1 = (seed + r * 0x9E3779B9) % 2 ** 32, (seed // 2 ** 32 + r * 0xBB67AE85) % 2 ** 32
             h0, l0 = _mulhilo(0xD2511F53, x0)
