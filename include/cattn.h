@@ -487,6 +487,69 @@ cattn_status cattn_swa_decode(const void* q, const void* k_cache, const void* v_
                               void* stream);
 size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, int window, int sinks, int dtype);
 
+/*
+ * Feed-forward operators of a decoder block: the gated projections and dropout,
+ * by the same conventions as the operators above.
+ *
+ * Gated projections of the rows of x [T, C] by w_gate and w_up [F, C] (one row per
+ * output column, no bias):
+ *     g = x w_gate^T,  u = x w_up^T,  h = act(g) * u        [T, F]
+ * T counts tokens: 1 or a few in serving, where the weights' bytes are the cost, or
+ * thousands.  Products are summed in float, h comes from the unrounded g and u, and
+ * each output is rounded once.
+ *
+ *   x, w_gate, w_up, h: `dtype`, contiguous
+ *   gate, up: out, [T, F] `dtype`: g and u for the backward; or both NULL
+ *   activation: CATTN_SILU: g / (1 + exp(-g)); CATTN_GELU: the tanh form,
+ *             0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
+ * Supported: C and F multiples of 8 and at most 2^18; T * C and T * F at most 2^33.
+ * Tensors 16-byte aligned.  A size of 0 is an empty problem (nothing is written,
+ * h for C = 0 neither).  A row of x reaches its own rows of h, gate and up only.
+ */
+typedef enum { CATTN_SILU = 0, CATTN_GELU = 1 } cattn_activation;
+
+cattn_status cattn_gated_fwd(const void* x, const void* w_gate, const void* w_up, void* h, void* gate, void* up, int T,
+                             int C, int F, int activation, int dtype, void* stream);
+
+/* Backward for upstream dh [T, F], with the forward's gate and up:
+ *     dg = dh * u * act'(g),  du = dh * act(g)
+ *     dx = dg w_gate + du w_up          [T, C]
+ *     dw_gate = dg^T x,  dw_up = du^T x [F, C]
+ * all `dtype`.  dg and du are rounded to `dtype` (they are operands of the
+ * products); sums are float.  workspace: at least
+ * cattn_gated_bwd_workspace_bytes(T, C, F, dtype) bytes, 16-byte aligned. */
+cattn_status cattn_gated_bwd(const void* x, const void* w_gate, const void* w_up, const void* gate, const void* up,
+                             const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, int T, int C, int F,
+                             int activation, int dtype, void* stream);
+size_t cattn_gated_bwd_workspace_bytes(int T, int C, int F, int dtype);
+
+/*
+ * Dropout of n contiguous elements, with the residual's addition, its mask from a
+ * counter-based generator and never stored:
+ *     y_i = residual_i + (x_i / (1 - p) if kept else 0)     (residual NULL: 0)
+ * Element i is kept iff w_i >= round(p 2^32), w_i word i % 4 of Philox-4x32 with
+ * ten rounds, key `seed` (low word first), counter words (i / 4, site, step mod
+ * 2^32, step / 2^32).  The mask depends on these numbers alone: the backward, given
+ * the same ones, makes it again, and different sites (the places of a model that
+ * drop) or steps have masks of their own.
+ *
+ *   x, residual, y: `dtype`, 16-byte aligned; y may be x or residual (the same
+ *             address), or else shares no element with them
+ *   p:        in [0, 1 - 2^-32]
+ *   step_at:  DEVICE, or NULL: *step_at (read when the kernel runs) is added to
+ *             step, modulo 2^64, so that a captured graph drops anew at each replay
+ * What x holds at a dropped element does not matter.  1 / (1 - p) is a float; the
+ * sum is rounded once to float and once to `dtype`.  Supported: n at most 2^33.
+ */
+cattn_status cattn_dropout_fwd(const void* x, const void* residual, void* y, long long n, double p,
+                               unsigned long long seed, unsigned site, unsigned long long step, const long long* step_at,
+                               int dtype, void* stream);
+
+/* Backward: dx_i = dy_i / (1 - p) if kept else 0, with the forward's p, seed, site
+ * and step; the residual's gradient is dy itself.  dx may be dy. */
+cattn_status cattn_dropout_bwd(const void* dy, void* dx, long long n, double p, unsigned long long seed, unsigned site,
+                               unsigned long long step, const long long* step_at, int dtype, void* stream);
+
 /* Bytes of workspace cattn_attn_bwd needs: 2 * B * H * Sp * sizeof(float),
  * Sp = S rounded up to a multiple of 32 (0 for an empty or invalid shape). */
 size_t cattn_bwd_workspace_bytes(int B, int H, int S, int D);

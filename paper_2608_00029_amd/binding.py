@@ -31,7 +31,9 @@ EXPORTED = ("cattn_attn_fwd", "cattn_attn_bwd", "cattn_attn_fwd_ex", "cattn_attn
             "cattn_gelu_bwd", "cattn_sce_fwd", "cattn_sce_bwd", "cattn_attn_bwd_noalloc",
             "cattn_rmsnorm_fwd", "cattn_rmsnorm_fwd_q8", "cattn_rmsnorm_bwd", "cattn_rmsnorm_bwd_workspace_bytes",
             "cattn_rope_frequencies", "cattn_rope", "cattn_rope_append", "cattn_swa_fwd", "cattn_swa_bwd",
-            "cattn_swa_bwd_workspace_bytes", "cattn_swa_decode", "cattn_swa_decode_workspace_bytes")
+            "cattn_swa_bwd_workspace_bytes", "cattn_swa_decode", "cattn_swa_decode_workspace_bytes",
+            "cattn_gated_fwd", "cattn_gated_bwd", "cattn_gated_bwd_workspace_bytes", "cattn_dropout_fwd",
+            "cattn_dropout_bwd")
 
 
 class CattnError(RuntimeError):
@@ -113,6 +115,17 @@ def lib() -> ctypes.CDLL:
         L.cattn_swa_decode.restype = i
         L.cattn_swa_decode_workspace_bytes.argtypes = [i] * 8
         L.cattn_swa_decode_workspace_bytes.restype = ctypes.c_size_t
+        ull, ui = ctypes.c_ulonglong, ctypes.c_uint
+        L.cattn_gated_fwd.argtypes = [vp] * 6 + [i] * 5 + [vp]
+        L.cattn_gated_fwd.restype = i
+        L.cattn_gated_bwd.argtypes = [vp] * 10 + [i] * 5 + [vp]
+        L.cattn_gated_bwd.restype = i
+        L.cattn_gated_bwd_workspace_bytes.argtypes = [i] * 4
+        L.cattn_gated_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.cattn_dropout_fwd.argtypes = [vp] * 3 + [ll, d, ull, ui, ull, vp, i, vp]
+        L.cattn_dropout_fwd.restype = i
+        L.cattn_dropout_bwd.argtypes = [vp] * 2 + [ll, d, ull, ui, ull, vp, i, vp]
+        L.cattn_dropout_bwd.restype = i
         L.cattn_status_string.argtypes = [i]
         L.cattn_status_string.restype = ctypes.c_char_p
         L.cattn_last_error_string.argtypes = []
