@@ -172,37 +172,6 @@ __global__ __launch_bounds__(256, 2) void ffn_tile_kernel(TileArgs<T> g) {
     }
 }
 
-// dg = dh u act'(g), du = dh act(g), eight elements a thread.
-template <typename T>
-__global__ __launch_bounds__(256) void ffn_slopes_kernel(const T* __restrict__ gate, const T* __restrict__ up,
-                                                         const T* __restrict__ dh, T* __restrict__ dg,
-                                                         T* __restrict__ du, int64_t n8, bool gelu) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n8) return;
-  typedef T t8 __attribute__((ext_vector_type(8)));
-  const t8 g = ((const t8*)gate)[i], u = ((const t8*)up)[i], d = ((const t8*)dh)[i];
-  t8 a, b;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float act, slope;
-    act_and_slope<sizeof(T) == 4>((float)g[e], gelu, act, slope);
-    a[e] = (T)((float)d[e] * (float)u[e] * slope);
-    b[e] = (T)((float)d[e] * act);
-  }
-  ((t8*)dg)[i] = a;
-  ((t8*)du)[i] = b;
-}
-
-template <typename T> static hipError_t slopes(const GatedBwd& a, hipStream_t st) {
-  const int64_t n = (int64_t)a.T * a.F, n8 = n / 8;
-  hipLaunchKernelGGL(ffn_slopes_kernel<T>, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st, (const T*)a.gate,
-                     (const T*)a.up, (const T*)a.dh, (T*)a.ws, (T*)a.ws + n, n8, a.gelu);
-  return hipGetLastError();
-}
-hipError_t launch_gated_slopes(const GatedBwd& a, hipStream_t st) {
-  return a.bf16 ? slopes<__bf16>(a, st) : slopes<float>(a, st);
-}
-
 static unsigned tiles(int n, int t) { return (unsigned)((n - 1) / t + 1); }
 
 template <typename T> static hipError_t fwd(const GatedFwd& a, hipStream_t st) {
@@ -213,20 +182,18 @@ template <typename T> static hipError_t fwd(const GatedFwd& a, hipStream_t st) {
   return hipGetLastError();
 }
 template <typename T> static hipError_t bwd(const GatedBwd& a, hipStream_t st) {
-  hipError_t e = launch_gated_slopes(a, st);
-  if (e != hipSuccess) return e;
   const T *dg = (const T*)a.ws, *du = dg + (int64_t)a.T * a.F, *x = (const T*)a.x;
   const TileArgs<T> gx{{dg, du, a.F}, {(const T*)a.wg, (const T*)a.wu, a.C}, a.T, a.C, a.F,
                        (T*)a.dx, nullptr, nullptr, nullptr, a.gelu};
   hipLaunchKernelGGL((ffn_tile_kernel<T, DX>), dim3(tiles(a.C, TILE) * tiles(a.T, TILE)), dim3(256), 0, st, gx);
-  e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const TileArgs<T> gw{{dg, du, a.F}, {x, x, a.C}, a.F, a.C, a.T, (T*)a.dwg, (T*)a.dwu, nullptr, nullptr, a.gelu};
   hipLaunchKernelGGL((ffn_tile_kernel<T, DW>), dim3(2 * tiles(a.C, TILE) * tiles(a.F, TILE)), dim3(256), 0, st, gw);
   return hipGetLastError();
 }
 
-hipError_t launch_gated_fwd(const GatedFwd& a, hipStream_t st) { return a.bf16 ? fwd<__bf16>(a, st) : fwd<float>(a, st); }
-hipError_t launch_gated_bwd(const GatedBwd& a, hipStream_t st) { return a.bf16 ? bwd<__bf16>(a, st) : bwd<float>(a, st); }
+hipError_t launch_gated_fwd_f32(const GatedFwd& a, hipStream_t st) { return fwd<float>(a, st); }
+hipError_t launch_gated_bwd_f32(const GatedBwd& a, hipStream_t st) { return bwd<float>(a, st); }
 
 }  // namespace cattn

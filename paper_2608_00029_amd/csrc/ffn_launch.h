@@ -30,8 +30,11 @@ struct GatedBwd {
 inline size_t gated_bwd_bytes(int T, int F, bool bf16) { return 2 * (size_t)T * F * (bf16 ? 2 : 4); }
 hipError_t launch_gated_fwd(const GatedFwd& a, hipStream_t st);
 hipError_t launch_gated_bwd(const GatedBwd& a, hipStream_t st);
-// dg = dh u act'(g), du = dh act(g) into a.ws
-hipError_t launch_gated_slopes(const GatedBwd& a, hipStream_t st);
+// The products alone: of the forward; of the backward, from dg and du in a.ws
+hipError_t launch_gated_fwd_f32(const GatedFwd& a, hipStream_t st);
+hipError_t launch_gated_bwd_f32(const GatedBwd& a, hipStream_t st);
+hipError_t launch_gated_fwd_bf16(const GatedFwd& a, hipStream_t st);
+hipError_t launch_gated_bwd_bf16(const GatedBwd& a, hipStream_t st);
 
 // ---------------------------------------------------------------------------
 // Dropout
