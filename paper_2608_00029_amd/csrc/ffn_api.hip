@@ -63,7 +63,7 @@ cattn_status cattn_gated_fwd(const void* x, const void* w_gate, const void* w_up
 
 size_t cattn_gated_bwd_workspace_bytes(int T, int C, int F, int dtype) {
   if (T <= 0 || C <= 0 || F <= 0 || !valid_dtype(dtype) || !gated_supported(T, C, F)) return 0;
-  return gated_bwd_bytes(T, F, dtype == CATTN_BF16);
+  return gated_bwd_bytes(T, C, F, dtype == CATTN_BF16);
 }
 
 cattn_status cattn_gated_bwd(const void* x, const void* w_gate, const void* w_up, const void* gate, const void* up,

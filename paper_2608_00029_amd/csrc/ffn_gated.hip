@@ -36,6 +36,7 @@ template <typename T> static hipError_t slopes(const GatedBwd& a, hipStream_t st
   return hipGetLastError();
 }
 hipError_t launch_gated_fwd(const GatedFwd& a, hipStream_t st) {
+  if (gated_rows_columns(a.T, a.F, a.bf16)) return launch_gated_rows(a, st);
   return a.bf16 ? launch_gated_fwd_bf16(a, st) : launch_gated_fwd_f32(a, st);
 }
 hipError_t launch_gated_bwd(const GatedBwd& a, hipStream_t st) {

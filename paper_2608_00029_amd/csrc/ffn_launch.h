@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "ffn_sched.h"
+
 namespace cattn {
 
 // ---------------------------------------------------------------------------
@@ -23,13 +25,17 @@ struct GatedFwd {
 struct GatedBwd {
   const void *x, *wg, *wu, *gate, *up, *dh;
   void *dx, *dwg, *dwu;  // [T, C], [F, C], [F, C]
-  void* ws;              // dg, then du: [T, F] of the tensors' type each
+  void* ws;              // dg, then du: [T, F] of the tensors' type each; then partial sums (floats)
   int T, C, F;
   bool gelu, bf16;
 };
-inline size_t gated_bwd_bytes(int T, int F, bool bf16) { return 2 * (size_t)T * F * (bf16 ? 2 : 4); }
+inline size_t gated_bwd_bytes(int T, int C, int F, bool bf16) {  // (T F is a multiple of 8: the floats are aligned)
+  return 2 * (size_t)T * F * (bf16 ? 2 : 4) + 4 * (size_t)ffn_part_floats(T, C, F, bf16);
+}
 hipError_t launch_gated_fwd(const GatedFwd& a, hipStream_t st);
 hipError_t launch_gated_bwd(const GatedBwd& a, hipStream_t st);
+// The forward of few rows (gated_rows_columns)
+hipError_t launch_gated_rows(const GatedFwd& a, hipStream_t st);
 // The products alone: of the forward; of the backward, from dg and du in a.ws
 hipError_t launch_gated_fwd_f32(const GatedFwd& a, hipStream_t st);
 hipError_t launch_gated_bwd_f32(const GatedBwd& a, hipStream_t st);

@@ -1,0 +1,83 @@
+// Which form of the tile kernel a gated projection's product takes, and into how many
+// parts its sum over k is cut (host only; tests ask it too).
+#pragma once
+
+#include <stdint.h>
+
+namespace cattn {
+
+enum { FWD, DX, DW };
+
+// A form: a tile of p x q, and what it costs, in us, measured: a work group's chunk of
+// 128 bytes of k with every compute unit at work, and a tile's start and end.  `at_once`:
+// work groups on the GPU at a time (256 compute units).
+//
+// Large tiles pay least for their operands' way through L2 and LDS, smaller ones leave
+// fewer compute units idle in the last round and at the edges.  Rates reached, bfloat16
+// (forward 4096 x 4096 x 10240, TFLOP/s): 256 x 256 1255 to 1303, 192 x 256 1176,
+// 128 x 128 960, two work groups of them a compute unit, or 875, one with four chunks
+// ahead in place of two, which is what few work groups need to keep HBM busy (24 x 4096 x
+// 10240: 38.6 us, with two ahead 53.9).
+struct FfnForm {
+  int id, p, q, at_once;
+  float chunk, tile;
+};
+enum { F256, F192, F128, F128DEEP, F64X128, F64 };
+constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 256, 1.30f, 3.f},
+                                {F128, 128, 128, 512, 1.05f, 3.f}, {F128DEEP, 128, 128, 256, 0.60f, 2.5f}};
+// float32: what bounds every form is the matrix cores' rate, and a compute unit's work
+// groups share it, so that rounds are counted by compute units.
+constexpr FfnForm kFfnF32[] = {{F64X128, 64, 128, 256, 1.05f, 3.f}, {F64, 64, 64, 256, 0.58f, 2.f}};
+
+struct FfnPlan {
+  int form, parts;
+};
+
+// M x N sums over K (dx: over two halves of K), two of them for dW.  The forward is not
+// cut: its sums meet in the activation.
+inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
+  const int64_t chunk = bf16 ? 64 : 32, n = (K + chunk - 1) / chunk * (mode == DX ? 2 : 1);
+  FfnPlan best{0, 1};
+  float best_us = 1e30f;
+  const FfnForm* forms = bf16 ? kFfnBf16 : kFfnF32;
+  for (int i = 0; i < (bf16 ? 4 : 2); ++i) {
+    const FfnForm& f = forms[i];
+    if (mode == FWD && f.id == F64) continue;  // (a gate and an up column of 64 each are 128 rows of the weights)
+    const int64_t q = mode == FWD ? f.q / 2 : f.q;
+    const int64_t tiles = ((M + f.p - 1) / f.p) * ((N + q - 1) / q) * (mode == DW ? 2 : 1);
+    for (int parts = 1; parts <= (mode == FWD ? 1 : 32) && n >= 4 * (parts - 1); parts *= 2) {
+      const int64_t rounds = (tiles * parts + f.at_once - 1) / f.at_once, each = (n + parts - 1) / parts;
+      float us = (float)rounds * ((float)each * f.chunk + f.tile);
+      // parts: a launch, and their floats out and in at 4 TB/s
+      if (parts > 1) us += 4.f + 2e-6f * (float)(parts * M * N * (mode == DW ? 2 : 1));
+      if (us < best_us) {
+        best_us = us;
+        best = FfnPlan{f.id, parts};
+      }
+    }
+  }
+  return best;
+}
+
+// Columns of h that a work group of the forward's few-rows kernel takes; 0: the tiles take
+// the call.  More columns read x less often, fewer make work groups enough.  us, 8 / 16 /
+// 32 columns / tiles:
+//   bfloat16  1 x 4096 x 10240  32.2 / 33.3 / 46.8 / 36.1    16 x 1600 x 4288  10.7 / 10.8 /  9.5 / 11.5
+//             8 x 4096 x 10240  37.4 / 35.2 /    - /    -    24 x 2048 x 5632  16.5 / 17.1 / 13.2 / 13.4
+//            24 x 4096 x 10240  54.4 / 47.3 / 55.9 / 38.6    32 x 8192 x 1024  23.5 / 30.3 / 44.2 / 39.2
+//   float32   1 x 4096 x 10240  63.1 / 71.1 / 92.4           16 x 4096 x 10240 87.4 / 77.2 / 92.8
+constexpr int kGatedRows = 32;
+inline int gated_rows_columns(int T, int F, bool bf16) {
+  if (T > kGatedRows || (bf16 && T > 8 && F >= 8192)) return 0;
+  if (!bf16 || T <= 8) return T > 4 && F >= 8192 ? 16 : 8;
+  return F >= 4096 ? 32 : 8;
+}
+
+// Floats of partial sums that a backward's products leave (one after the other, in one place).
+inline int64_t ffn_part_floats(int64_t T, int64_t C, int64_t F, bool bf16) {
+  const int dx = ffn_plan(DX, T, C, F, bf16).parts, dw = ffn_plan(DW, F, C, T, bf16).parts;
+  const int64_t a = dx > 1 ? dx * T * C : 0, b = dw > 1 ? 2 * dw * F * C : 0;
+  return a > b ? a : b;
+}
+
+}  // namespace cattn
