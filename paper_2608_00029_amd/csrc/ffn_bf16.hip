@@ -9,10 +9,10 @@ template <int MODE> struct LaunchBf16 {
     const FfnPlan plan = ffn_plan(MODE, g.M, g.N, g.K, true);
     g.parts = plan.parts;
     switch (plan.form) {
-      case F256: return launch_form<bf16, MODE, 4, 2, 2, 4, 2>(g, st);
-      case F192: return launch_form<bf16, MODE, 2, 4, 3, 2, 2>(g, st);
-      case F128: return launch_form<bf16, MODE, 4, 2, 1, 2, 2>(g, st);
-      case F128DEEP: return launch_form<bf16, MODE, 4, 2, 1, 2, 4>(g, st);
+      case F256: return launch_form<bf16, MODE, 4, 2, 2, 4, 2, 1>(g, st);
+      case F192: return launch_form<bf16, MODE, 2, 4, 3, 2, 2, 1>(g, st);
+      case F128: return launch_form<bf16, MODE, 4, 2, 1, 2, 2, 1>(g, st);
+      case F128DEEP: return launch_form<bf16, MODE, 4, 2, 1, 2, 4, 3>(g, st);
     }
     return hipErrorInvalidValue;
   }

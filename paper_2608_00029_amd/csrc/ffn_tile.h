@@ -30,21 +30,22 @@ namespace cattn {
 
 static __device__ __attribute__((aligned(16))) const unsigned kZeros[4] = {0, 0, 0, 0};
 
-// A 16-byte piece of an operand's row and the contraction of two of them, one k-step.
+// A 16-byte piece of an operand's row, and the contraction of two of them, one k-step of
+// N matrix instructions.
 // A lane L = 32 h + r holds piece h of the step's two, of row r.
 template <typename T> struct Step;
 template <> struct Step<bf16> {
   typedef bf16x8 frag;
-  static __device__ __forceinline__ f32x16 run(frag a, frag b, f32x16 c) {
+  static constexpr int N = 1;
+  static __device__ __forceinline__ f32x16 run(frag a, frag b, f32x16 c, int) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
 };
 template <> struct Step<float> {
   typedef f32x4 frag;
-  static __device__ __forceinline__ f32x16 run(frag a, frag b, f32x16 c) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-    return c;
+  static constexpr int N = 4;
+  static __device__ __forceinline__ f32x16 run(frag a, frag b, f32x16 c, int j) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
   }
 };
 
@@ -80,18 +81,19 @@ template <typename T> struct TileArgs {
   bool gelu;
 };
 
-// WP x WQ waves of TP x TQ blocks of 32 x 32; NS: chunks that are copied ahead.
-template <int WP, int WQ, int TP, int TQ, int NS> struct Form {
+// WP x WQ waves of TP x TQ blocks of 32 x 32; NS: chunks that are copied ahead; AHEAD (1
+// or 3): k-steps that fragments are read ahead.
+template <int WP, int WQ, int TP, int TQ, int NS, int AHEAD> struct Form {
   static constexpr int W = WP * WQ, P = 32 * WP * TP, Q = 32 * WQ * TQ;
   static constexpr int kLds = ((NS + 1) * P + NS * Q) * 128;
   // work groups of a compute unit: by LDS, by 16 waves
   static constexpr int kPerCu = 160 * 1024 / kLds * W <= 16 ? 160 * 1024 / kLds : 16 / W;
 };
 
-template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS>
-__global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS>::kPerCu * WP * WQ / 4)) void ffn_tile_kernel(TileArgs<T> g) {
+template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS, int AHEAD>
+__global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS, AHEAD>::kPerCu * WP * WQ / 4)) void ffn_tile_kernel(TileArgs<T> g) {
   static_assert(MODE != FWD || TQ % 2 == 0, "a wave has a column's gate and up");
-  typedef Form<WP, WQ, TP, TQ, NS> Fm;
+  typedef Form<WP, WQ, TP, TQ, NS, AHEAD> Fm;
   typedef Step<T> St;
   constexpr int KC = 128 / sizeof(T), E = 16 / sizeof(T), KS = 2 * E;  // k of a chunk, a piece, a step
   constexpr int W = Fm::W, P = Fm::P, Q = Fm::Q, NSP = NS + 1, NSQ = NS;  // LDS slots of the operands' chunks
@@ -139,7 +141,9 @@ __global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS>::kPerCu * W
   constexpr int HALVES = MODE == DX ? 2 : 1;
   const int whole = g.K / KC, rest = g.K % KC != 0;
   const int n_chunks = HALVES * (whole + rest);
-  auto first_of = [&](int part) { return (int)((int64_t)n_chunks * part / g.parts); };
+  auto first_of = [&](int part) {  // (uniform; the division leaves it in a vector register)
+    return __builtin_amdgcn_readfirstlane((int)((int64_t)n_chunks * part / g.parts));
+  };
 
   // What is copied next: chunk `at` of item k_cp's, which end at `to_at`, from src for
   // `left` more chunks.
@@ -271,16 +275,18 @@ __global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS>::kPerCu * W
       return v;
     }
   };
-  frag pf[2][TP], qf[2][TQ];
-  // Fragment f (p's first) of k-step s of the present chunk, into buffer s % 2.
+  static_assert(AHEAD == 1 || AHEAD == 3, "a chunk is four steps");
+  constexpr int NBUF = AHEAD + 1;
+  frag pf[NBUF][TP], qf[NBUF][TQ];
+  // Fragment f (p's first) of k-step s of the present chunk, into buffer s % NBUF.
   auto read_frag = [&](auto s, auto f) __attribute__((always_inline)) {
     constexpr int S = decltype(s)::value, t = decltype(f)::value, a = t - TP;
     if constexpr (t < TP) {
-      if constexpr (P_ACROSS) pf[S % 2][t] = read_across(fp[t], IC<P>{}, s);
-      else pf[S % 2][t] = *(const frag*)(smem + (rp ^ (S * 32)) + t * 4096);
+      if constexpr (P_ACROSS) pf[S % NBUF][t] = read_across(fp[t], IC<P>{}, s);
+      else pf[S % NBUF][t] = *(const frag*)(smem + (rp ^ (S * 32)) + t * 4096);
     } else {
-      if constexpr (Q_ACROSS) qf[S % 2][a] = read_across(fq[a], IC<Q>{}, s);
-      else qf[S % 2][a] = *(const frag*)(smem + (rq ^ (S * 32)) + a * 4096);
+      if constexpr (Q_ACROSS) qf[S % NBUF][a] = read_across(fq[a], IC<Q>{}, s);
+      else qf[S % NBUF][a] = *(const frag*)(smem + (rq ^ (S * 32)) + a * 4096);
     }
   };
   // The bases to the next chunk's slots.
@@ -311,7 +317,10 @@ __global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS>::kPerCu * W
 
   wait_vm((NS - 1) * NC);
   asm volatile("s_barrier" ::: "memory");
-  unroll<TP + TQ>([&](auto f) { read_frag(IC<0>{}, f); });
+  auto read_first = [&]() __attribute__((always_inline)) {  // the steps of a chunk that are read before it begins
+    unroll<AHEAD>([&](auto s) { unroll<TP + TQ>([&](auto f) { read_frag(s, f); }); });
+  };
+  read_first();
   for (int k = 0; k < n_mine; ++k) {
     const Item it = item_at(k);
     const bool second = MODE == DW && it.pt >= g.n_pt;
@@ -325,20 +334,22 @@ __global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS>::kPerCu * W
 #pragma unroll
       for (int a = 0; a < TQ; ++a) acc[t][a] = f32x16{};
 
-    // k-step S: a contraction first, so that the matrix core has work while the next
-    // step's fragments are asked for, two after each of the first contractions; copies
-    // FROM .. TO - 1 after the others.
-    auto step = [&](auto s, auto from, auto to) __attribute__((always_inline)) {
-      constexpr int S = decltype(s)::value, FROM = decltype(from)::value, COPIES = decltype(to)::value - FROM;
-      constexpr int STEPS = TP * TQ, READS = TP + TQ, PER = READS > 2 * STEPS ? READS : 2;
+    // k-step S: a contraction first, so that the matrix core has work while the fragments
+    // AHEAD steps on are asked for, two after each of the first contractions; after the
+    // others, before the meeting its share of p's copies, behind it of q's.
+    auto step = [&](auto s) __attribute__((always_inline)) {
+      constexpr int S = decltype(s)::value, MEET = 4 - AHEAD;
+      constexpr int FROM = S < MEET ? CP * S / MEET : CP + CQ * (S - MEET) / AHEAD;
+      constexpr int COPIES = (S < MEET ? CP * (S + 1) / MEET : CP + CQ * (S + 1 - MEET) / AHEAD) - FROM;
+      constexpr int STEPS = St::N * TP * TQ, READS = TP + TQ, PER = READS > 2 * STEPS ? READS : 2;
       constexpr int READ_STEPS = (READS + PER - 1) / PER, LEFT = STEPS - READ_STEPS + 1;
       unroll<STEPS>([&](auto n) {
-        constexpr int N = decltype(n)::value, t = N / TQ, a = N % TQ;
-        acc[t][a] = St::run(pf[S % 2][t], qf[S % 2][a], acc[t][a]);
+        constexpr int N = decltype(n)::value, t = N / TQ % TP, a = N % TQ;
+        acc[t][a] = St::run(pf[S % NBUF][t], qf[S % NBUF][a], acc[t][a], N / (TP * TQ));
         __builtin_amdgcn_sched_barrier(0);
         unroll<PER>([&](auto f) {
           constexpr int F = N * PER + decltype(f)::value;
-          if constexpr (F < READS) read_frag(IC<(S + 1) % 4>{}, IC<F>{});
+          if constexpr (F < READS) read_frag(IC<(S + AHEAD) % 4>{}, IC<F>{});
         });
         constexpr int at_n = N - READ_STEPS + 1, before = at_n < 0 ? 0 : at_n * COPIES / LEFT,
                       after = at_n < 0 ? 0 : (at_n + 1) * COPIES / LEFT;
@@ -359,63 +370,91 @@ __global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS>::kPerCu * W
     };
     for (int c = 0; c < n_chunks_k; ++c) {
       if (active) {
-        // p's part of the chunk NS ahead, into the slot of the chunk before
-        step(IC<0>{}, IC<0>{}, IC<CP / 3>{});
-        step(IC<1>{}, IC<CP / 3>{}, IC<CP * 2 / 3>{});
-        step(IC<2>{}, IC<CP * 2 / 3>{}, IC<CP>{});
-        meet();
-        // q's, into this chunk's
-        step(IC<3>{}, IC<CP>{}, IC<NC>{});  // (after the last chunk of all its reads are discarded)
+        // p's part of the chunk NS ahead goes into the slot of the chunk before, q's, after
+        // the meeting, into this chunk's.  (After the last chunk of all the reads are discarded.)
+        unroll<4>([&](auto s) {
+          if constexpr (decltype(s)::value == 4 - AHEAD) meet();
+          step(s);
+        });
       } else {
 #pragma unroll
         for (int i = 0; i < CP; ++i) copy(i);
         meet();
 #pragma unroll
         for (int i = CP; i < NC; ++i) copy(i);
-        unroll<TP + TQ>([&](auto f) { read_frag(IC<0>{}, f); });
+        read_first();
       }
       copied();
     }
 
-    // acc[t][a][e]: row p0 + 32 t + acc_row(e, h), block a's column r
+    // acc[t][a][e]: row p0 + 32 t + acc_row(e, h), block a's column r.  Rows are stored in
+    // pairs, e and e + 1: of one column a lane and two bytes each, neighbouring lanes first
+    // exchange values so that each has four bytes of one row.
     if (active) {
-      T* out = second ? g.out1 : g.out0;
-      float* part = g.part + ((int64_t)it.part * (MODE == DW ? 2 : 1) + second) * g.M * g.N;
-#pragma unroll
-      for (int t = 0; t < TP; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int m = p0 + 32 * t + acc_row(e, h);
-          if constexpr (MODE == FWD) {
-            typedef T cols __attribute__((ext_vector_type(NP)));
-            const int n = q0 + r * NP;
-            if (m < g.M && n < g.N) {  // (N is a multiple of 8)
-              const int64_t o = (int64_t)m * g.N + n;
-              cols hv, gv, uv;
-#pragma unroll
-              for (int a = 0; a < NP; ++a) {
-                const float ga = acc[t][a][e], u = acc[t][NP + a][e];
-                hv[a] = (T)(act_of<sizeof(T) == 4>(ga, g.gelu) * u);
-                gv[a] = (T)ga;
-                uv[a] = (T)u;
-              }
-              *(cols*)(out + o) = hv;
-              if (g.gate) {
-                *(cols*)(g.gate + o) = gv;
-                *(cols*)(g.up + o) = uv;
-              }
-            }
+      // (Hidden from the compiler, which else forms every row's address before the loop and
+      // has no registers for them.)
+      int N = g.N;
+      asm volatile("" : "+s"(N));
+      const int64_t first = (int64_t)p0 * N + q0;
+      T* out = (second ? g.out1 : g.out0) + first;
+      float* part = g.part + ((int64_t)it.part * (MODE == DW ? 2 : 1) + second) * g.M * N + first;
+      constexpr bool SWAP = sizeof(T) == 2;
+      const int odd = SWAP ? r & 1 : 0;
+      auto put = [&](auto full) __attribute__((always_inline)) {
+        constexpr bool FULL = decltype(full)::value;
+        // cols of NV columns from column c of the wave's on, rows e and e + 1
+        auto put_pair = [&](auto* to, int row, int c, auto v0, auto v1) __attribute__((always_inline)) {
+          typedef std::remove_reference_t<decltype(*to)> E1;
+          constexpr int NV = sizeof(v0) / sizeof(E1);
+          if constexpr (NV == 1 && sizeof(E1) == 2) {
+            const unsigned own = __builtin_bit_cast(unsigned short, (E1)v0[0]) |
+                                 (unsigned)__builtin_bit_cast(unsigned short, (E1)v1[0]) << 16;
+            const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)own, 0xB1, 0xf, 0xf, true);  // lane ^ 1's
+            const unsigned both = odd ? __builtin_amdgcn_perm(own, other, 0x07060302u)
+                                      : __builtin_amdgcn_perm(other, own, 0x05040100u);
+            const int64_t at = (int64_t)row * N + c;
+            if (FULL || (p0 + row + 4 * h + odd < g.M && q0 + c + r - odd < N))
+              *(unsigned*)((char*)(to + at) + (unsigned)(((4 * h + odd) * N + r - odd) * (int)sizeof(E1))) = both;
           } else {
 #pragma unroll
-            for (int a = 0; a < TQ; ++a) {
-              const int n = q0 + 32 * a + r;
-              if (m < g.M && n < g.N) {
-                if (g.parts > 1) part[(int64_t)m * g.N + n] = acc[t][a][e];
-                else out[(int64_t)m * g.N + n] = (T)acc[t][a][e];
-              }
-            }
+            for (int k = 0; k < 2; ++k)
+              if (FULL || (p0 + row + k + 4 * h < g.M && q0 + c + r * NV < N))
+                *(decltype(v0)*)((char*)(to + (int64_t)(row + k) * N + c) +
+                                 (unsigned)((4 * h * N + r * NV) * (int)sizeof(E1))) = k ? v1 : v0;
           }
-        }
+        };
+        unroll<TP * 8>([&](auto n) {
+          constexpr int t = decltype(n)::value / 8, e = decltype(n)::value % 8 * 2, row = 32 * t + 8 * (e >> 2) + (e & 3);
+          if constexpr (MODE == FWD) {  // (N is a multiple of 8: a lane's columns all belong to h, or none)
+            typedef T cols __attribute__((ext_vector_type(NP)));
+            cols hv[2], gv[2], uv[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int a = 0; a < NP; ++a) {
+                const float ga = acc[t][a][e + k], u = acc[t][NP + a][e + k];
+                hv[k][a] = (T)(act_of<sizeof(T) == 4>(ga, g.gelu) * u);
+                gv[k][a] = (T)ga;
+                uv[k][a] = (T)u;
+              }
+            put_pair(out, row, 0, hv[0], hv[1]);
+            if (g.gate) {
+              put_pair(g.gate + first, row, 0, gv[0], gv[1]);
+              put_pair(g.up + first, row, 0, uv[0], uv[1]);
+            }
+          } else {
+            unroll<TQ>([&](auto ac) {
+              constexpr int a = decltype(ac)::value;
+              typedef T one __attribute__((ext_vector_type(1)));
+              typedef float onef __attribute__((ext_vector_type(1)));
+              if (g.parts > 1) put_pair(part, row, 32 * a, onef{acc[t][a][e]}, onef{acc[t][a][e + 1]});
+              else put_pair(out, row, 32 * a, one{(T)acc[t][a][e]}, one{(T)acc[t][a][e + 1]});
+            });
+          }
+        });
+      };
+      if (p0 + 32 * TP <= g.M && q0 + NT / WQ <= N) put(IC<1>{});
+      else put(IC<0>{});
     }
   }
   wait_vm(0);  // no copy may land in this LDS once another work group has it
@@ -451,15 +490,20 @@ inline int cus_per_xcd() {
   return cached[dev];
 }
 
-template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS>
+template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS, int AHEAD>
 static hipError_t launch_form(TileArgs<T> g, hipStream_t st) {
-  typedef Form<WP, WQ, TP, TQ, NS> Fm;
+  typedef Form<WP, WQ, TP, TQ, NS, AHEAD> Fm;
   constexpr int NT = MODE == FWD ? Fm::Q / 2 : Fm::Q;
   g.n_pt = (g.M - 1) / Fm::P + 1;
   g.n_qt = (g.N - 1) / NT + 1;
   const int64_t items = (int64_t)g.n_pt * g.n_qt * (MODE == DW ? 2 : 1) * g.parts;
-  const int64_t per_xcd = std::min<int64_t>((items + kXcdGroup - 1) / kXcdGroup, cus_per_xcd() * Fm::kPerCu);
-  hipLaunchKernelGGL((ffn_tile_kernel<T, MODE, WP, WQ, TP, TQ, NS>), dim3((unsigned)(per_xcd * kXcdGroup)), dim3(64 * Fm::W), 0, st, g);
+  // Work groups of a compute unit: no more than an even spread needs.  LDS beyond what a
+  // work group uses keeps the hardware from putting more on some units and fewer on others.
+  // (float32 dW of 2048 x 768 x 2048, 768 items of 64 x 64 on 256 units: 119 us without, - with.)
+  const int per_cu = (int)std::min<int64_t>((items - 1) / (cus_per_xcd() * kXcdGroup) + 1, Fm::kPerCu);
+  const unsigned more_lds = per_cu < Fm::kPerCu ? (160 * 1024 / per_cu - Fm::kLds) & ~1023u : 0;
+  const int64_t per_xcd = std::min<int64_t>((items + kXcdGroup - 1) / kXcdGroup, cus_per_xcd() * per_cu);
+  hipLaunchKernelGGL((ffn_tile_kernel<T, MODE, WP, WQ, TP, TQ, NS, AHEAD>), dim3((unsigned)(per_xcd * kXcdGroup)), dim3(64 * Fm::W), more_lds, st, g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts == 1) return e;
   const int64_t n4 = (int64_t)g.M * g.N / 4;
