@@ -11,8 +11,8 @@ template <int MODE> struct LaunchBf16 {
     switch (plan.form) {
       case F256: return launch_form<bf16, MODE, 4, 2, 2, 4, 2, 1>(g, st);
       case F192: return launch_form<bf16, MODE, 2, 4, 3, 2, 2, 1>(g, st);
-      case F128: return launch_form<bf16, MODE, 4, 2, 1, 2, 2, 1>(g, st);
-      case F128DEEP: return launch_form<bf16, MODE, 4, 2, 1, 2, 4, 3>(g, st);
+      case F256X128: return launch_form<bf16, MODE, 4, 2, 2, 2, 2, 1>(g, st);
+      case F128: return launch_form<bf16, MODE, 4, 2, 1, 2, 4, 3>(g, st);
     }
     return hipErrorInvalidValue;
   }

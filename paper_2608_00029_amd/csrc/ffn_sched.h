@@ -9,25 +9,31 @@ namespace cattn {
 enum { FWD, DX, DW };
 
 // A form: a tile of p x q, and what it costs, in us, measured: a work group's chunk of
-// 128 bytes of k with every compute unit at work, and a tile's start and end.  `at_once`:
-// work groups on the GPU at a time (256 compute units).
+// 128 bytes of k with every compute unit at work, and a tile's start and end.
 //
-// Large tiles pay least for their operands' way through L2 and LDS, smaller ones leave
-// fewer compute units idle in the last round and at the edges.  Rates reached, bfloat16
-// (forward 4096 x 4096 x 10240, TFLOP/s): 256 x 256 1255 to 1303, 192 x 256 1176,
-// 128 x 128 960, two work groups of them a compute unit, or 875, one with four chunks
-// ahead in place of two, which is what few work groups need to keep HBM busy (24 x 4096 x
-// 10240: 38.6 us, with two ahead 53.9).
+// Large tiles pay least for their operands' way through L2 and LDS (a compute unit takes
+// about 60 bytes a ns), smaller ones leave fewer compute units idle in the last round and
+// at the edges.  bfloat16, us:             256 x 256  192 x 256  256 x 128  128 x 128
+//   forward  4096 x 4096 x 10240               572        592        630        758
+//            3777 x 1024 x 2728                 59         52         58         71
+//            1024 x 1024 x 2728                 29         26         21         23
+//   dW       3777 x 1024 x 2728                 80         66         56         69
+//   dx       3777 x 1024 x 2728                107         85         75         57
+// The smallest has four chunks ahead in place of two, which is what few work groups need to
+// keep HBM busy (24 x 4096 x 10240: 38.6 us, with two ahead 53.9), and reads fragments three
+// steps ahead (200 x 2048 x 5632: 18.8, one step 21.2; 256 x 128 loses by it, 630 to 738).
 struct FfnForm {
-  int id, p, q, at_once;
+  int id, p, q;
   float chunk, tile;
 };
-enum { F256, F192, F128, F128DEEP, F64X128, F64 };
-constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 256, 1.30f, 3.f},
-                                {F128, 128, 128, 512, 1.05f, 3.f}, {F128DEEP, 128, 128, 256, 0.60f, 2.5f}};
-// float32: what bounds every form is the matrix cores' rate, and a compute unit's work
-// groups share it, so that rounds are counted by compute units.
-constexpr FfnForm kFfnF32[] = {{F64X128, 64, 128, 256, 1.05f, 3.f}, {F64, 64, 64, 256, 0.58f, 2.f}};
+enum { F256, F192, F256X128, F128, F64X128, F64 };
+constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 1.30f, 3.f},
+                                {F256X128, 256, 128, 0.94f, 3.f}, {F128, 128, 128, 0.60f, 2.5f}};
+// float32: the matrix cores' rate bounds both forms, and a compute unit's work groups share
+// it.  (64 x 128 / 64 x 64, us: dW of 2048 x 768 x 2048 135 / 113, of 4096 x 1024 x 2728 393 /
+// 436.)
+constexpr FfnForm kFfnF32[] = {{F64X128, 64, 128, 1.05f, 3.f}, {F64, 64, 64, 0.58f, 2.f}};
+constexpr int kFfnUnits = 256;  // compute units
 
 struct FfnPlan {
   int form, parts;
@@ -46,7 +52,7 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
     const int64_t q = mode == FWD ? f.q / 2 : f.q;
     const int64_t tiles = ((M + f.p - 1) / f.p) * ((N + q - 1) / q) * (mode == DW ? 2 : 1);
     for (int parts = 1; parts <= (mode == FWD ? 1 : 32) && n >= 4 * (parts - 1); parts *= 2) {
-      const int64_t rounds = (tiles * parts + f.at_once - 1) / f.at_once, each = (n + parts - 1) / parts;
+      const int64_t rounds = (tiles * parts + kFfnUnits - 1) / kFfnUnits, each = (n + parts - 1) / parts;
       float us = (float)rounds * ((float)each * f.chunk + f.tile);
       // parts: a launch, and their floats out and in at 4 TB/s
       if (parts > 1) us += 4.f + 2e-6f * (float)(parts * M * N * (mode == DW ? 2 : 1));
