@@ -502,7 +502,7 @@ size_t cattn_swa_decode_workspace_bytes(int B, int Hq, int Hkv, int cap, int D, 
  *   gate, up: out, [T, F] `dtype`: g and u for the backward; or both NULL
  *   activation: CATTN_SILU: g / (1 + exp(-g)); CATTN_GELU: the tanh form,
  *             0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
- * Supported: C and F multiples of 8 and at most 2^18; T * C and T * F at most 2^33.
+ * Supported: C and F multiples of 8 and at most 2^18; T * C, T * F and F * C at most 2^33.
  * Tensors 16-byte aligned.  A size of 0 is an empty problem (nothing is written,
  * h for C = 0 neither).  A row of x reaches its own rows of h, gate and up only.
  */

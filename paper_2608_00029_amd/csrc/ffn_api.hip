@@ -17,7 +17,7 @@ size_t size_of(int dtype) { return dtype == CATTN_BF16 ? 2 : 4; }
 // Of a shape without a 0.
 bool gated_supported(int T, int C, int F) {
   return C % 8 == 0 && F % 8 == 0 && C <= kFfnMaxW && F <= kFfnMaxW && (int64_t)T * C <= kFfnMaxElements &&
-         (int64_t)T * F <= kFfnMaxElements;
+         (int64_t)T * F <= kFfnMaxElements && (int64_t)F * C <= kFfnMaxElements;
 }
 
 cattn_status check_gated(int T, int C, int F, int activation, int dtype) {
@@ -27,7 +27,7 @@ cattn_status check_gated(int T, int C, int F, int activation, int dtype) {
   if (activation != CATTN_SILU && activation != CATTN_GELU)
     return fail(CATTN_ERR_INVALID_ARG, "activation must be CATTN_SILU or CATTN_GELU");
   if (T == 0 || C == 0 || F == 0 || gated_supported(T, C, F)) return CATTN_OK;
-  return fail(CATTN_ERR_UNSUPPORTED, "C and F must be multiples of 8 and at most 2^18, T * C and T * F at most 2^33");
+  return fail(CATTN_ERR_UNSUPPORTED, "C and F must be multiples of 8 and at most 2^18, T * C, T * F and F * C at most 2^33");
 }
 
 cattn_status check_tensors(const void* const* p, int n) {

@@ -14,7 +14,7 @@ namespace cattn {
 // Gated projections: g = x Wg^T, u = x Wu^T, h = act(g) u
 // ---------------------------------------------------------------------------
 constexpr int kFfnMaxW = 1 << 18;                    // columns, C and F
-constexpr int64_t kFfnMaxElements = int64_t(1) << 33;  // of one tensor: T C, T F; dropout's n
+constexpr int64_t kFfnMaxElements = int64_t(1) << 33;  // of one tensor: T C, T F, F C; dropout's n
 
 struct GatedFwd {
   const void *x, *wg, *wu;  // [T, C], [F, C], [F, C]

@@ -54,8 +54,8 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
     for (int parts = 1; parts <= (mode == FWD ? 1 : 32) && n >= 4 * (parts - 1); parts *= 2) {
       const int64_t rounds = (tiles * parts + kFfnUnits - 1) / kFfnUnits, each = (n + parts - 1) / parts;
       float us = (float)rounds * ((float)each * f.chunk + f.tile);
-      // parts: a launch, and their floats out and in at 4 TB/s
-      if (parts > 1) us += 4.f + 2e-6f * (float)(parts * M * N * (mode == DW ? 2 : 1));
+      // parts: another kernel, and their floats out and in at 4 TB/s
+      if (parts > 1) us += 6.f + 2e-6f * (float)(parts * M * N * (mode == DW ? 2 : 1));
       if (us < best_us) {
         best_us = us;
         best = FfnPlan{f.id, parts};

@@ -40,7 +40,7 @@ def dropout_bwd(dy=P[0], dx=P[2], n=100, p=0.1, seed=1, site=2, step=3, at=P[3],
     (gated, dict(T=-1), BAD), (gated, dict(C=-8), BAD), (gated, dict(F=-8), BAD), (gated, dict(dtype=2), BAD),
     (gated, dict(act=2), BAD), (gated, dict(act=-1), BAD), (gated, dict(C=60), NO), (gated, dict(F=36), NO),
     (gated, dict(C=(1 << 18) + 8), NO), (gated, dict(F=(1 << 18) + 8), NO), (gated, dict(T=1 << 30, C=16, F=8), NO),
-    (gated, dict(T=1 << 30, C=8, F=16), NO), (gated, dict(x=0), BAD), (gated, dict(wg=0), BAD), (gated, dict(wu=0), BAD),
+    (gated, dict(T=1 << 30, C=8, F=16), NO), (gated, dict(T=1, C=1 << 17, F=(1 << 16) + 8), NO), (gated, dict(x=0), BAD), (gated, dict(wg=0), BAD), (gated, dict(wu=0), BAD),
     (gated, dict(h=0), BAD), (gated, dict(gate=0), BAD), (gated, dict(up=0), BAD), (gated, dict(x=P[0] + 8), BAD),
     (gated, dict(gate=P[4] + 2), BAD), (gated, dict(h=P[0]), BAD), (gated, dict(h=P[1] + 4080), BAD), (gated, dict(gate=P[5] + 16), BAD),
     (gated, dict(up=P[3] + 240), BAD), (gated, dict(gate=P[2]), BAD),
