@@ -9,9 +9,10 @@ template <int MODE> struct LaunchF32 {
     const FfnPlan plan = ffn_plan(MODE, g.M, g.N, g.K, false);
     g.parts = plan.parts;
     switch (plan.form) {
-      case F64X128: return launch_form<float, MODE, 2, 2, 1, 2, 2, 3>(g, st);
+      case F128: return launch_form<float, MODE, 2, 2, 2, 2, 2, 1>(g, st);
+      case F64X128: return launch_form<float, MODE, 2, 2, 1, 2, 2, 1>(g, st);
       case F64:
-        if constexpr (MODE != FWD) return launch_form<float, MODE, 2, 2, 1, 1, 2, 3>(g, st);
+        if constexpr (MODE != FWD) return launch_form<float, MODE, 2, 2, 1, 1, 2, 1>(g, st);
     }
     return hipErrorInvalidValue;
   }

@@ -29,10 +29,12 @@ struct FfnForm {
 enum { F256, F192, F256X128, F128, F64X128, F64 };
 constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 1.30f, 3.f},
                                 {F256X128, 256, 128, 0.94f, 3.f}, {F128, 128, 128, 0.60f, 2.5f}};
-// float32: the matrix cores' rate bounds both forms, and a compute unit's work groups share
-// it.  (64 x 128 / 64 x 64, us: dW of 2048 x 768 x 2048 135 / 113, of 4096 x 1024 x 2728 393 /
-// 436.)
-constexpr FfnForm kFfnF32[] = {{F64X128, 64, 128, 1.05f, 3.f}, {F64, 64, 64, 0.58f, 2.f}};
+// float32: the matrix cores' rate bounds all forms, and a compute unit's work groups share
+// it.  us:                    128 x 128  64 x 128  64 x 64
+//   dW  2048 x 768 x 2048         127       130      106
+//   dx  4096 x 1024 x 2728        342       354      375
+//   dW  4096 x 1024 x 2728        492       375      418
+constexpr FfnForm kFfnF32[] = {{F128, 128, 128, 1.98f, 4.f}, {F64X128, 64, 128, 1.03f, 2.5f}, {F64, 64, 64, 0.53f, 2.f}};
 constexpr int kFfnUnits = 256;  // compute units
 
 struct FfnPlan {
@@ -46,7 +48,7 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
   FfnPlan best{0, 1};
   float best_us = 1e30f;
   const FfnForm* forms = bf16 ? kFfnBf16 : kFfnF32;
-  for (int i = 0; i < (bf16 ? 4 : 2); ++i) {
+  for (int i = 0; i < (bf16 ? 4 : 3); ++i) {
     const FfnForm& f = forms[i];
     if (mode == FWD && f.id == F64) continue;  // (a gate and an up column of 64 each are 128 rows of the weights)
     const int64_t q = mode == FWD ? f.q / 2 : f.q;

@@ -22,7 +22,8 @@ CASES = [
     (15896, 264, 264, "bf16"), (33, 8520, 136, "bf16"), (3002, 32, 2064, "bf16"), (12871, 4168, 200, "bf16"), (572, 11424, 40, "bf16"),
     (132, 1040, 7904, "bf16"), (17124, 136, 40, "bf16"), (8963, 32, 848, "bf16"), (17086, 528, 40, "bf16"), (193, 4272, 11400, "bf16"),
     # float32
-    (300, 72, 40, "f32"), (363, 40, 168, "f32"), (35, 8312, 40, "f32"), (1784, 2064, 32, "f32"), (8476, 72, 40, "f32"), (33, 1072, 3984, "f32"),
+    (300, 72, 40, "f32"), (494, 40, 264, "f32"), (35, 8312, 40, "f32"), (67, 8224, 32, "f32"), (33, 8480, 72, "f32"), (16640, 72, 32, "f32"),
+    (21293, 72, 800, "f32"), (5747, 3232, 32, "f32"), (67, 3136, 5632, "f32"), (33, 3200, 5968, "f32"),
 ]
 
 
