@@ -10,10 +10,10 @@
 // as they are; operands stored across k lie as [k][row] and are read by the transposing
 // LDS reads, so that no transposed copy is made.
 //
-// The matrix cores bound it, if they are fed: k streams in chunks of a line, 128 bytes, p's through three LDS slots and q's through two, copied up to two chunks
-// ahead, across tiles; operand fragments are read one k-step of 16 ahead, also across
-// chunks; a chunk has one barrier, and copies and fragment reads sit between
-// contractions.  Work groups walk their chiplet's tiles (eight row tiles by some column
+// The matrix cores bound it, if they are fed: k streams in chunks of a line, 128 bytes,
+// p's through NS + 1 LDS slots and q's through NS, copied ahead, across tiles; operand
+// fragments are read a k-step (16 bfloat16, 8 floats) or three ahead, also across chunks;
+// a chunk has one barrier, and copies and fragment reads sit between contractions.  Work groups walk their chiplet's tiles (eight row tiles by some column
 // tiles at a time, so that what is in flight on it fits its L2).  Ends: rows past the
 // end are read from the last one and not stored; pieces of a chunk past the end of k
 // come from a line of zeros.
@@ -77,7 +77,8 @@ template <typename T> struct TileArgs {
   T *out0, *out1, *gate, *up;
   float* part;                    // parts > 1: sums over a part of k, [parts][dW: 2][M][N]
   int n_pt, n_qt;                 // tiles of p (dW: of dWg), of q
-  int parts;                      // of k, an item each
+  int parts;                      // of k, an item each: part_chunks chunks, and one more for the
+  int part_chunks, part_more;     // first part_more of them
   bool gelu;
 };
 
@@ -91,17 +92,18 @@ template <int WP, int WQ, int TP, int TQ, int NS, int AHEAD> struct Form {
 };
 
 template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS, int AHEAD>
-__global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS, AHEAD>::kPerCu * WP * WQ / 4)) void ffn_tile_kernel(TileArgs<T> g) {
+__global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS, AHEAD>::kPerCu * WP * WQ / 4))
+void ffn_tile_kernel(TileArgs<T> g) {
   static_assert(MODE != FWD || TQ % 2 == 0, "a wave has a column's gate and up");
   typedef Form<WP, WQ, TP, TQ, NS, AHEAD> Fm;
   typedef Step<T> St;
   constexpr int KC = 128 / sizeof(T), E = 16 / sizeof(T), KS = 2 * E;  // k of a chunk, a piece, a step
   constexpr int W = Fm::W, P = Fm::P, Q = Fm::Q, NSP = NS + 1, NSQ = NS;  // LDS slots of the operands' chunks
   constexpr bool P_ACROSS = MODE == DW, Q_ACROSS = MODE != FWD;
-  constexpr int PB = P * 128, QB = Q * 128;                        // bytes of a chunk
+  constexpr int PB = P * 128, QB = Q * 128;    // bytes of a chunk
   constexpr int CP = (PB / 1024 + W - 1) / W, CQ = (QB / 1024 + W - 1) / W, NC = CP + CQ;  // copies of a wave and chunk
-  constexpr int NT = MODE == FWD ? Q / 2 : Q;                                      // columns of the result
-  constexpr int NP = TQ / 2;                                                       // forward: 32-column blocks of h
+  constexpr int NT = MODE == FWD ? Q / 2 : Q;  // columns of the result
+  constexpr int NP = TQ / 2;                   // forward: 32-column blocks of h
   __shared__ __attribute__((aligned(16))) char smem[Fm::kLds];
 
   // This work group's items (a tile and a part of k): begin + l, begin + l + per_xcd, ...
@@ -140,10 +142,7 @@ __global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS, AHEAD>::kPe
   // Chunks of a tile: for each half of k its whole ones and one for the rest.
   constexpr int HALVES = MODE == DX ? 2 : 1;
   const int whole = g.K / KC, rest = g.K % KC != 0;
-  const int n_chunks = HALVES * (whole + rest);
-  auto first_of = [&](int part) {  // (uniform; the division leaves it in a vector register)
-    return __builtin_amdgcn_readfirstlane((int)((int64_t)n_chunks * part / g.parts));
-  };
+  auto first_of = [&](int part) { return part * g.part_chunks + imin(part, g.part_more); };
 
   // What is copied next: chunk `at` of item k_cp's, which end at `to_at`, from src for
   // `left` more chunks.
@@ -217,7 +216,7 @@ __global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS, AHEAD>::kPe
     }
   };
   point();
-#pragma unroll
+#pragma unroll 1  // (less code to fetch: the smallest products are little else)
   for (int c = 0; c < NS; ++c) {
 #pragma unroll
     for (int i = 0; i < NC; ++i) copy(i);
@@ -497,13 +496,13 @@ static hipError_t launch_form(TileArgs<T> g, hipStream_t st) {
   g.n_pt = (g.M - 1) / Fm::P + 1;
   g.n_qt = (g.N - 1) / NT + 1;
   const int64_t items = (int64_t)g.n_pt * g.n_qt * (MODE == DW ? 2 : 1) * g.parts;
-  // Work groups of a compute unit: no more than an even spread needs.  LDS beyond what a
-  // work group uses keeps the hardware from putting more on some units and fewer on others.
-  // (float32 dW of 2048 x 768 x 2048, 768 items of 64 x 64 on 256 units: 119 us without, - with.)
-  const int per_cu = (int)std::min<int64_t>((items - 1) / (cus_per_xcd() * kXcdGroup) + 1, Fm::kPerCu);
-  const unsigned more_lds = per_cu < Fm::kPerCu ? (160 * 1024 / per_cu - Fm::kLds) & ~1023u : 0;
-  const int64_t per_xcd = std::min<int64_t>((items + kXcdGroup - 1) / kXcdGroup, cus_per_xcd() * per_cu);
-  hipLaunchKernelGGL((ffn_tile_kernel<T, MODE, WP, WQ, TP, TQ, NS, AHEAD>), dim3((unsigned)(per_xcd * kXcdGroup)), dim3(64 * Fm::W), more_lds, st, g);
+  const int64_t per_xcd = std::min<int64_t>((items + kXcdGroup - 1) / kXcdGroup, cus_per_xcd() * Fm::kPerCu);
+  constexpr int KC = 128 / sizeof(T);
+  const int n_chunks = ((g.K - 1) / KC + 1) * (MODE == DX ? 2 : 1);
+  g.part_chunks = n_chunks / g.parts;
+  g.part_more = n_chunks % g.parts;
+  hipLaunchKernelGGL((ffn_tile_kernel<T, MODE, WP, WQ, TP, TQ, NS, AHEAD>), dim3((unsigned)(per_xcd * kXcdGroup)),
+                     dim3(64 * Fm::W), 0, st, g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts == 1) return e;
   const int64_t n4 = (int64_t)g.M * g.N / 4;
@@ -515,7 +514,7 @@ static hipError_t launch_form(TileArgs<T> g, hipStream_t st) {
 // The products of a forward and a backward, each by LAUNCH<MODE>::run(args, stream).
 template <typename T, template <int> class LAUNCH> static hipError_t tiles_fwd(const GatedFwd& a, hipStream_t st) {
   return LAUNCH<FWD>::run(TileArgs<T>{(const T*)a.x, nullptr, (const T*)a.wg, (const T*)a.wu, a.C, a.C, a.T, a.F, a.C,
-                                      (T*)a.h, nullptr, (T*)a.gate, (T*)a.up, nullptr, 0, 0, 1, a.gelu},
+                                      (T*)a.h, nullptr, (T*)a.gate, (T*)a.up, nullptr, 0, 0, 1, 0, 0, a.gelu},
                           st);
 }
 template <typename T, template <int> class LAUNCH> static hipError_t tiles_bwd(const GatedBwd& a, hipStream_t st) {
@@ -523,11 +522,11 @@ template <typename T, template <int> class LAUNCH> static hipError_t tiles_bwd(c
   const T *dg = (const T*)a.ws, *du = dg + n, *x = (const T*)a.x;
   float* part = (float*)((T*)a.ws + 2 * n);
   const hipError_t e = LAUNCH<DX>::run(TileArgs<T>{dg, du, (const T*)a.wg, (const T*)a.wu, a.F, a.C, a.T, a.C, a.F,
-                                                   (T*)a.dx, nullptr, nullptr, nullptr, part, 0, 0, 1, a.gelu},
+                                                   (T*)a.dx, nullptr, nullptr, nullptr, part, 0, 0, 1, 0, 0, a.gelu},
                                        st);
   if (e != hipSuccess) return e;
   return LAUNCH<DW>::run(TileArgs<T>{dg, du, x, x, a.F, a.C, a.F, a.C, a.T, (T*)a.dwg, (T*)a.dwu, nullptr, nullptr, part,
-                                     0, 0, 1, a.gelu},
+                                     0, 0, 1, 0, 0, a.gelu},
                          st);
 }
 
