@@ -70,15 +70,18 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
 // Columns of h that a work group of the forward's few-rows kernel takes; 0: the tiles take
 // the call.  More columns read x less often, fewer make work groups enough.  us, 8 / 16 /
 // 32 columns / tiles:
-//   bfloat16  1 x 4096 x 10240  32.2 / 33.3 / 46.8 / 36.1    16 x 1600 x 4288  10.7 / 10.8 /  9.5 / 11.5
-//             8 x 4096 x 10240  37.4 / 35.2 /    - /    -    24 x 2048 x 5632  16.5 / 17.1 / 13.2 / 13.4
-//            24 x 4096 x 10240  54.4 / 47.3 / 55.9 / 38.6    32 x 8192 x 1024  23.5 / 30.3 / 44.2 / 39.2
-//   float32   1 x 4096 x 10240  63.1 / 71.1 / 92.4           16 x 4096 x 10240 87.4 / 77.2 / 92.8
+//   bfloat16  1 x 4096 x 10240  32.2 / 33.3 / 46.8 / 36.1    16 x 1600 x 4288  10.6 / 10.7 /  9.7 / 12.4
+//             8 x 4096 x 10240  36.9 / 35.9 / 47.7 / 38.1    24 x 2048 x 5632  16.4 / 16.4 / 12.9 / 15.2
+//             8 x 5120 x 13824  65.6 / 60.8 / 61.4 / 54.0    32 x 8192 x 1024  23.5 / 30.3 / 44.2 / 39.2
+//            24 x 4096 x 10240  55.0 / 48.2 / 53.6 / 37.8    32 x 1024 x 4096   8.3 /  8.2 /  8.5 / 10.0
+//   float32   1 x 4096 x 10240  63.1 / 71.1                  16 x 4096 x 10240 87.4 / 77.2
+//             1 x 1600 x 4288   13.7 / 16.2                  16 x 1600 x 4288  19.2 / 19.2
 constexpr int kGatedRows = 32;
 inline int gated_rows_columns(int T, int F, bool bf16) {
-  if (T > kGatedRows || (bf16 && T > 8 && F >= 8192)) return 0;
-  if (!bf16 || T <= 8) return T > 4 && F >= 8192 ? 16 : 8;
-  return F >= 4096 ? 32 : 8;
+  if (T > kGatedRows) return 0;
+  if (!bf16) return T > 4 && F >= 8192 ? 16 : 8;
+  if (F >= 8192) return T > 4 ? 0 : 8;
+  return T > 8 && F >= 4096 ? 32 : 8;
 }
 
 // Floats of partial sums that a backward's products leave (one after the other, in one place).
