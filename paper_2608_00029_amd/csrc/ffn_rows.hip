@@ -142,9 +142,8 @@ template <typename T, int RF> static hipError_t launch_nx(const GatedFwd& a, hip
 }
 template <typename T> static hipError_t launch_rf(const GatedFwd& a, hipStream_t st) {
   const int rf = gated_rows_columns(a.T, a.F, a.bf16);
-  if constexpr (sizeof(T) == 2)
-    if (rf == 32) return launch_nx<T, 32>(a, st);
-  return rf == 16 ? launch_nx<T, 16>(a, st) : launch_nx<T, 8>(a, st);
+  constexpr int MORE = sizeof(T) == 2 ? 32 : 16;
+  return rf == MORE ? launch_nx<T, MORE>(a, st) : launch_nx<T, 8>(a, st);
 }
 
 hipError_t launch_gated_rows(const GatedFwd& a, hipStream_t st) {

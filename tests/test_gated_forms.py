@@ -53,9 +53,7 @@ def forms_of(case, p):
     return {fwd, (dtype, "dx", NAMES[xf], xp > 1), (dtype, "dw", NAMES[wf], wp > 1)}
 
 
-# (16 columns a work group are for at most eight tokens, bfloat16's 32 for more)
-EVERY = {(d, "rows", n, many) for d in ("bf16", "f32") for n in (8, 16, 32) for many in (False, True)
-         if (d, n) != ("f32", 32) and (n, many) != (16, True)} \
+EVERY = {(d, "rows", n, many) for d, n in (("bf16", 8), ("bf16", 32), ("f32", 8), ("f32", 16)) for many in (False, True)} \
     | {("bf16", "fwd", n, False) for n in NAMES[:4]} | {("f32", "fwd", n, False) for n in NAMES[3:5]} \
     | {("bf16", p, n, parts) for p in ("dx", "dw") for n in NAMES[:4] for parts in (False, True)} \
     | {("f32", p, n, parts) for p in ("dx", "dw") for n in NAMES[3:] for parts in (False, True)}
