@@ -13,10 +13,18 @@
 // The matrix cores bound it, if they are fed: k streams in chunks of a line, 128 bytes,
 // p's through NS + 1 LDS slots and q's through NS, copied ahead, across tiles; operand
 // fragments are read a k-step (16 bfloat16, 8 floats) or three ahead, also across chunks;
-// a chunk has one barrier, and copies and fragment reads sit between contractions.  Work groups walk their chiplet's tiles (eight row tiles by some column
-// tiles at a time, so that what is in flight on it fits its L2).  Ends: rows past the
-// end are read from the last one and not stored; pieces of a chunk past the end of k
-// come from a line of zeros.
+// a chunk has one barrier, and copies and fragment reads sit between contractions.  Work
+// groups walk their chiplet's tiles, four row tiles by some column tiles at a time, so that
+// what is in flight on it fits its L2.  Ends: rows past the end are read from the last one
+// and not stored; pieces of a chunk past the end of k come from a line of zeros.
+//
+// Rates reached, bfloat16, 256 x 256 tiles: 4096 x 4096 x 10240 522 us forward (1317
+// TFLOP/s), 504 dx, 527 dW, where the matrix cores are busy 72% of the cycles and the clock
+// is down to 1.5 - 1.9 GHz by power.  Found on the way there (forward, that size, us): chunks
+// of 64 bytes, half lines, 587, whole lines 527; fragments asked for before a k-step's first
+// contraction 587, after it 566; the same work without any copy 466, without the barrier too
+// 461; every line in L2 530 where 567 were then measured; four waves of 96 x 128 619 where
+// eight took 592.
 #pragma once
 
 #include <algorithm>
@@ -27,6 +35,11 @@
 #include "ffn_sched.h"
 
 namespace cattn {
+
+// Row tiles that a chiplet takes side by side.  (4 / 6 / 8 / 16, us: forward 4096 x 4096 x
+// 10240 522 / 532 / 533 / 540, 8192 x 1600 x 4288 218 / 217 / 221 / 229, dW of 2048 x 2048 x
+// 5632 104 / 104 / 107 / 108.)
+constexpr int kGroup = 4;
 
 static __device__ __attribute__((aligned(16))) const unsigned kZeros[4] = {0, 0, 0, 0};
 
@@ -130,10 +143,10 @@ void ffn_tile_kernel(TileArgs<T> g) {
       const int item = begin + l + imin(win + lane, n_mine - 1) * per_xcd;
       win_part = item / n_tiles;
       const int t = item - win_part * n_tiles;
-      const int group = t / (8 * g.n_qt), in = t - group * 8 * g.n_qt;
-      const int rows = imin(8, n_pt - 8 * group);
+      const int group = t / (kGroup * g.n_qt), in = t - group * kGroup * g.n_qt;
+      const int rows = imin(kGroup, n_pt - kGroup * group);
       win_q = in / rows;
-      win_p = 8 * group + in - win_q * rows;
+      win_p = kGroup * group + in - win_q * rows;
     }
     return Item{__builtin_amdgcn_readlane(win_p, k - win), __builtin_amdgcn_readlane(win_q, k - win),
                 __builtin_amdgcn_readlane(win_part, k - win)};
