@@ -11,8 +11,9 @@ template <int MODE> struct LaunchF32 {
     switch (plan.form) {
       case F128: return launch_form<float, MODE, 2, 2, 2, 2, 2, 1>(g, st);
       case F64X128: return launch_form<float, MODE, 2, 2, 1, 2, 2, 1>(g, st);
-      case F64:
-        if constexpr (MODE != FWD) return launch_form<float, MODE, 2, 2, 1, 1, 2, 1>(g, st);
+      case F64:  // (a gate and an up column in one wave: two waves beside each other, so two sets)
+        if constexpr (MODE == FWD) return launch_form<float, MODE, 2, 1, 1, 2, 2, 1, 2>(g, st);
+        else return launch_form<float, MODE, 2, 2, 1, 1, 2, 1>(g, st);
     }
     return hipErrorInvalidValue;
   }

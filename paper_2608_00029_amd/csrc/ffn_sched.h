@@ -34,6 +34,8 @@ constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 1
 //   dW  2048 x 768 x 2048         127       130      106
 //   dx  4096 x 1024 x 2728        342       354      375
 //   dW  4096 x 1024 x 2728        492       375      418
+//   forward  100 x 2048 x 4096              71       42
+//            300 x 1024 x 2048              38       39
 constexpr FfnForm kFfnF32[] = {{F128, 128, 128, 1.98f, 4.f}, {F64X128, 64, 128, 1.03f, 2.5f}, {F64, 64, 64, 0.53f, 2.f}};
 constexpr int kFfnUnits = 256;  // compute units
 
@@ -50,7 +52,6 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
   const FfnForm* forms = bf16 ? kFfnBf16 : kFfnF32;
   for (int i = 0; i < (bf16 ? 4 : 3); ++i) {
     const FfnForm& f = forms[i];
-    if (mode == FWD && f.id == F64) continue;  // (a gate and an up column of 64 each are 128 rows of the weights)
     const int64_t q = mode == FWD ? f.q / 2 : f.q;
     const int64_t tiles = ((M + f.p - 1) / f.p) * ((N + q - 1) / q) * (mode == DW ? 2 : 1);
     for (int parts = 1; parts <= (mode == FWD ? 1 : 32) && n >= 4 * (parts - 1); parts *= 2) {

@@ -96,19 +96,20 @@ template <typename T> struct TileArgs {
 };
 
 // WP x WQ waves of TP x TQ blocks of 32 x 32; NS: chunks that are copied ahead; AHEAD (1
-// or 3): k-steps that fragments are read ahead.
-template <int WP, int WQ, int TP, int TQ, int NS, int AHEAD> struct Form {
-  static constexpr int W = WP * WQ, P = 32 * WP * TP, Q = 32 * WQ * TQ;
-  static constexpr int kLds = ((NS + 1) * P + NS * Q) * 128;
+// or 3): k-steps that fragments are read ahead; WK: sets of such waves that share a chunk's
+// k-steps, their sums joined in LDS at the end (for few tiles: more waves a tile).
+template <int WP, int WQ, int TP, int TQ, int NS, int AHEAD, int WK = 1> struct Form {
+  static constexpr int W = WP * WQ * WK, P = 32 * WP * TP, Q = 32 * WQ * TQ;
+  static constexpr int kRing = ((NS + 1) * P + NS * Q) * 128, kLds = kRing + (WK - 1) * P * Q * 4;
   // work groups of a compute unit: by LDS, by 16 waves
   static constexpr int kPerCu = 160 * 1024 / kLds * W <= 16 ? 160 * 1024 / kLds : 16 / W;
 };
 
-template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS, int AHEAD>
-__global__ __launch_bounds__(64 * WP * WQ, (Form<WP, WQ, TP, TQ, NS, AHEAD>::kPerCu * WP * WQ / 4))
+template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS, int AHEAD, int WK = 1>
+__global__ __launch_bounds__(64 * WP * WQ * WK, (Form<WP, WQ, TP, TQ, NS, AHEAD, WK>::kPerCu * WP * WQ * WK / 4))
 void ffn_tile_kernel(TileArgs<T> g) {
   static_assert(MODE != FWD || TQ % 2 == 0, "a wave has a column's gate and up");
-  typedef Form<WP, WQ, TP, TQ, NS, AHEAD> Fm;
+  typedef Form<WP, WQ, TP, TQ, NS, AHEAD, WK> Fm;
   typedef Step<T> St;
   constexpr int KC = 128 / sizeof(T), E = 16 / sizeof(T), KS = 2 * E;  // k of a chunk, a piece, a step
   constexpr int W = Fm::W, P = Fm::P, Q = Fm::Q, NSP = NS + 1, NSQ = NS;  // LDS slots of the operands' chunks
@@ -130,7 +131,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
   if (n_mine <= 0) return;  // uniform over the group
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wp = w / WQ, wq = w % WQ;
+  const int wk = w / (WP * WQ), wp = w % (WP * WQ) / WQ, wq = w % WQ;
 
   // The items, 64 at a time, one per lane (the divisions run once for all of them).
   struct Item {
@@ -236,7 +237,9 @@ void ffn_tile_kernel(TileArgs<T> g) {
     copied();
   }
 
-  // Where this lane reads its operand fragments, of k-step 0 of the present chunk.
+  // Where this lane reads its operand fragments, of the first of its wave's NST k-steps of
+  // the present chunk.
+  constexpr int NST = 4 / WK;
   // (Stored across k: bfloat16 by two transposing reads of four k, at lo and hi; float by
   // four reads, one k each, from lo on.)
   struct Across {
@@ -245,6 +248,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
   auto across = [&](auto rows_c, int block) __attribute__((always_inline)) {  // image [KC][rows], 32 rows from 32 block on
     constexpr int rows = decltype(rows_c)::value;
     auto off = [&](int k, int row) {
+      k += wk * NST * KS;
       return (unsigned)(k * rows * (int)sizeof(T) + ((row / E ^ across_swz<T, rows>(k)) << 4) + row % E * (int)sizeof(T));
     };
     if constexpr (sizeof(T) == 2) {
@@ -261,7 +265,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
 #pragma unroll
     for (int t = 0; t < TP; ++t) fp[t] = across(IC<P>{}, wp * TP + t);
   } else {
-    rp = wp * TP * 4096 + r * 128 + ((h ^ row_swz(r)) << 4);
+    rp = (wp * TP * 4096 + r * 128 + ((h ^ row_swz(r)) << 4)) ^ (wk * NST * 32);
   }
   if constexpr (Q_ACROSS) {
 #pragma unroll
@@ -271,7 +275,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
       fq[a].hi += NSP * PB;
     }
   } else {
-    rq = NSP * PB + wq * TQ * 4096 + r * 128 + ((h ^ row_swz(r)) << 4);
+    rq = NSP * PB + ((wq * TQ * 4096 + r * 128 + ((h ^ row_swz(r)) << 4)) ^ (wk * NST * 32));
   }
   typedef typename St::frag frag;
   auto read_across = [&](Across f, auto rows, auto s) __attribute__((always_inline)) {
@@ -287,7 +291,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
       return v;
     }
   };
-  static_assert(AHEAD == 1 || AHEAD == 3, "a chunk is four steps");
+  static_assert(AHEAD < NST && (NST % (AHEAD + 1)) == 0, "buffers take turns");
   constexpr int NBUF = AHEAD + 1;
   frag pf[NBUF][TP], qf[NBUF][TQ];
   // Fragment f (p's first) of k-step s of the present chunk, into buffer s % NBUF.
@@ -350,7 +354,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
     // AHEAD steps on are asked for, two after each of the first contractions; after the
     // others, before the meeting its share of p's copies, behind it of q's.
     auto step = [&](auto s) __attribute__((always_inline)) {
-      constexpr int S = decltype(s)::value, MEET = 4 - AHEAD;
+      constexpr int S = decltype(s)::value, MEET = NST - AHEAD;
       constexpr int FROM = S < MEET ? CP * S / MEET : CP + CQ * (S - MEET) / AHEAD;
       constexpr int COPIES = (S < MEET ? CP * (S + 1) / MEET : CP + CQ * (S + 1 - MEET) / AHEAD) - FROM;
       constexpr int STEPS = St::N * TP * TQ, READS = TP + TQ, PER = READS > 2 * STEPS ? READS : 2;
@@ -361,7 +365,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
         __builtin_amdgcn_sched_barrier(0);
         unroll<PER>([&](auto f) {
           constexpr int F = N * PER + decltype(f)::value;
-          if constexpr (F < READS) read_frag(IC<(S + AHEAD) % 4>{}, IC<F>{});
+          if constexpr (F < READS) read_frag(IC<(S + AHEAD) % NST>{}, IC<F>{});
         });
         constexpr int at_n = N - READ_STEPS + 1, before = at_n < 0 ? 0 : at_n * COPIES / LEFT,
                       after = at_n < 0 ? 0 : (at_n + 1) * COPIES / LEFT;
@@ -384,8 +388,8 @@ void ffn_tile_kernel(TileArgs<T> g) {
       if (active) {
         // p's part of the chunk NS ahead goes into the slot of the chunk before, q's, after
         // the meeting, into this chunk's.  (After the last chunk of all the reads are discarded.)
-        unroll<4>([&](auto s) {
-          if constexpr (decltype(s)::value == 4 - AHEAD) meet();
+        unroll<NST>([&](auto s) {
+          if constexpr (decltype(s)::value == NST - AHEAD) meet();
           step(s);
         });
       } else {
@@ -399,10 +403,37 @@ void ffn_tile_kernel(TileArgs<T> g) {
       copied();
     }
 
+    if constexpr (WK > 1) {
+      // The other sets' sums, added in their order.  (They are read before the next meeting,
+      // and written again after it.)
+      f32x4* joint = (f32x4*)(smem + Fm::kRing);
+      constexpr int BLOCKS = TP * TQ * 4;
+      if (active && wk) {
+        f32x4* to = joint + (w - WP * WQ) * BLOCKS * 64 + lane;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+          const f32x16& v = acc[b / 4 / TQ][b / 4 % TQ];
+          to[b * 64] = f32x4{v[b % 4 * 4], v[b % 4 * 4 + 1], v[b % 4 * 4 + 2], v[b % 4 * 4 + 3]};
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): copies stay in flight
+      asm volatile("s_barrier" ::: "memory");
+      if (active && !wk) {
+#pragma unroll
+        for (int k2 = 0; k2 < WK - 1; ++k2)
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b) {
+            const f32x4 v = joint[((k2 * WP * WQ + w) * BLOCKS + b) * 64 + lane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[b / 4 / TQ][b / 4 % TQ][b % 4 * 4 + j] += v[j];
+          }
+      }
+    }
+
     // acc[t][a][e]: row p0 + 32 t + acc_row(e, h), block a's column r.  Rows are stored in
     // pairs, e and e + 1: of one column a lane and two bytes each, neighbouring lanes first
     // exchange values so that each has four bytes of one row.
-    if (active) {
+    if (active && wk == 0) {
       // (Hidden from the compiler, which else forms every row's address before the loop and
       // has no registers for them.)
       int N = g.N;
@@ -502,9 +533,9 @@ inline int cus_per_xcd() {
   return cached[dev];
 }
 
-template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS, int AHEAD>
+template <typename T, int MODE, int WP, int WQ, int TP, int TQ, int NS, int AHEAD, int WK = 1>
 static hipError_t launch_form(TileArgs<T> g, hipStream_t st) {
-  typedef Form<WP, WQ, TP, TQ, NS, AHEAD> Fm;
+  typedef Form<WP, WQ, TP, TQ, NS, AHEAD, WK> Fm;
   constexpr int NT = MODE == FWD ? Fm::Q / 2 : Fm::Q;
   g.n_pt = (g.M - 1) / Fm::P + 1;
   g.n_qt = (g.N - 1) / NT + 1;
@@ -514,7 +545,7 @@ static hipError_t launch_form(TileArgs<T> g, hipStream_t st) {
   const int n_chunks = ((g.K - 1) / KC + 1) * (MODE == DX ? 2 : 1);
   g.part_chunks = n_chunks / g.parts;
   g.part_more = n_chunks % g.parts;
-  hipLaunchKernelGGL((ffn_tile_kernel<T, MODE, WP, WQ, TP, TQ, NS, AHEAD>), dim3((unsigned)(per_xcd * kXcdGroup)),
+  hipLaunchKernelGGL((ffn_tile_kernel<T, MODE, WP, WQ, TP, TQ, NS, AHEAD, WK>), dim3((unsigned)(per_xcd * kXcdGroup)),
                      dim3(64 * Fm::W), 0, st, g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts == 1) return e;
