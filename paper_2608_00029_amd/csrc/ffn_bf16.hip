@@ -12,6 +12,10 @@ template <int MODE> struct LaunchBf16 {
       case F256: return launch_form<bf16, MODE, 4, 2, 2, 4, 2, 1>(g, st);
       case F192: return launch_form<bf16, MODE, 2, 4, 3, 2, 2, 1>(g, st);
       case F256X128: return launch_form<bf16, MODE, 4, 2, 2, 2, 2, 1>(g, st);
+      case F64: return launch_form<bf16, MODE, 2, 1, 1, 2, 4, 1, 2>(g, st);
+      case F128X64:
+        if constexpr (MODE == FWD) return launch_form<bf16, MODE, 4, 1, 1, 2, 3, 1, 2>(g, st);
+        break;
       case F128: return launch_form<bf16, MODE, 4, 2, 1, 2, 4, 3>(g, st);
     }
     return hipErrorInvalidValue;

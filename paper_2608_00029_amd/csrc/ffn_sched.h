@@ -22,13 +22,20 @@ enum { FWD, DX, DW };
 // The smallest has four chunks ahead in place of two, which is what few work groups need to
 // keep HBM busy (24 x 4096 x 10240: 38.6 us, with two ahead 53.9), and reads fragments three
 // steps ahead (200 x 2048 x 5632: 18.8, one step 21.2; 256 x 128 loses by it, 630 to 738).
+// Fewer tiles yet than compute units: a chunk's k-steps are shared by two sets of waves.
+//                                  128 x 128  128 x 64  64 x 64
+//   forward  200 x 2048 x 5632        17.2       22.2     25.5
+//            100 x 2048 x 5632        15.7       12.8     17.7
+//             64 x 2048 x 5632        15.1       12.3     10.9
+//             39 x 3272 x 3568        24.4       17.1     15.7
 struct FfnForm {
   int id, p, q;
   float chunk, tile;
 };
-enum { F256, F192, F256X128, F128, F64X128, F64 };
+enum { F256, F192, F256X128, F128, F64X128, F64, F128X64 };
 constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 1.30f, 3.f},
-                                {F256X128, 256, 128, 0.94f, 3.f}, {F128, 128, 128, 0.60f, 2.5f}};
+                                {F256X128, 256, 128, 0.94f, 3.f}, {F128, 128, 128, 0.60f, 2.5f},
+                                {F128X64, 128, 64, 0.31f, 2.9f},  {F64, 64, 64, 0.25f, 2.5f}};
 // float32: the matrix cores' rate bounds all forms, and a compute unit's work groups share
 // it.  us:                    128 x 128  64 x 128  64 x 64
 //   dW  2048 x 768 x 2048         127       130      106
@@ -50,8 +57,9 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
   FfnPlan best{0, 1};
   float best_us = 1e30f;
   const FfnForm* forms = bf16 ? kFfnBf16 : kFfnF32;
-  for (int i = 0; i < (bf16 ? 4 : 3); ++i) {
+  for (int i = 0; i < (bf16 ? 6 : 3); ++i) {
     const FfnForm& f = forms[i];
+    if (f.id == F128X64 && mode != FWD) continue;
     const int64_t q = mode == FWD ? f.q / 2 : f.q;
     const int64_t tiles = ((M + f.p - 1) / f.p) * ((N + q - 1) / q) * (mode == DW ? 2 : 1);
     for (int parts = 1; parts <= (mode == FWD ? 1 : 32) && n >= 4 * (parts - 1); parts *= 2) {

@@ -543,6 +543,7 @@ static hipError_t launch_form(TileArgs<T> g, hipStream_t st) {
   const int64_t per_xcd = std::min<int64_t>((items + kXcdGroup - 1) / kXcdGroup, cus_per_xcd() * Fm::kPerCu);
   constexpr int KC = 128 / sizeof(T);
   const int n_chunks = ((g.K - 1) / KC + 1) * (MODE == DX ? 2 : 1);
+  if (g.parts < 1 || g.parts > n_chunks) return hipErrorInvalidValue;  // (every item has a chunk: the kernel counts on it)
   g.part_chunks = n_chunks / g.parts;
   g.part_more = n_chunks % g.parts;
   hipLaunchKernelGGL((ffn_tile_kernel<T, MODE, WP, WQ, TP, TQ, NS, AHEAD, WK>), dim3((unsigned)(per_xcd * kXcdGroup)),
