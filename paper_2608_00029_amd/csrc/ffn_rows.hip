@@ -141,9 +141,10 @@ template <typename T, int RF> static hipError_t launch_nx(const GatedFwd& a, hip
   return a.T <= 16 ? launch<T, RF, 1>(a, st) : launch<T, RF, 2>(a, st);
 }
 template <typename T> static hipError_t launch_rf(const GatedFwd& a, hipStream_t st) {
-  const int rf = gated_rows_columns(a.T, a.F, a.bf16);
-  constexpr int MORE = sizeof(T) == 2 ? 32 : 16;
-  return rf == MORE ? launch_nx<T, MORE>(a, st) : launch_nx<T, 8>(a, st);
+  [[maybe_unused]] const int rf = gated_rows_columns(a.T, a.F, a.bf16);
+  if constexpr (sizeof(T) == 4)
+    if (rf == 16) return launch_nx<T, 16>(a, st);
+  return launch_nx<T, 8>(a, st);
 }
 
 hipError_t launch_gated_rows(const GatedFwd& a, hipStream_t st) {

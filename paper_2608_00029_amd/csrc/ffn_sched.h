@@ -34,8 +34,8 @@ struct FfnForm {
 };
 enum { F256, F192, F256X128, F128, F64X128, F64, F128X64 };
 constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 1.30f, 3.f},
-                                {F256X128, 256, 128, 0.94f, 3.f}, {F128, 128, 128, 0.60f, 2.5f},
-                                {F128X64, 128, 64, 0.31f, 2.9f},  {F64, 64, 64, 0.25f, 2.5f}};
+                                {F256X128, 256, 128, 0.94f, 3.f}, {F128, 128, 128, 0.56f, 2.5f},
+                                {F128X64, 128, 64, 0.31f, 2.9f},  {F64, 64, 64, 0.27f, 2.5f}};
 // float32: the matrix cores' rate bounds all forms, and a compute unit's work groups share
 // it.  us:                    128 x 128  64 x 128  64 x 64
 //   dW  2048 x 768 x 2048         127       130      106
@@ -77,20 +77,23 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
 }
 
 // Columns of h that a work group of the forward's few-rows kernel takes; 0: the tiles take
-// the call.  More columns read x less often, fewer make work groups enough.  us, 8 / 16 /
-// 32 columns / tiles:
-//   bfloat16  1 x 4096 x 10240  32.2 / 33.3 / 46.8 / 36.1    16 x 1600 x 4288  10.6 / 10.7 /  9.7 / 12.4
-//             8 x 4096 x 10240  36.9 / 35.9 / 47.7 / 38.1    24 x 2048 x 5632  16.4 / 16.4 / 12.9 / 15.2
-//             8 x 5120 x 13824  65.6 / 60.8 / 61.4 / 54.0    32 x 8192 x 1024  23.5 / 30.3 / 44.2 / 39.2
-//            24 x 4096 x 10240  55.0 / 48.2 / 53.6 / 37.8    32 x 1024 x 4096   8.3 /  8.2 /  8.5 / 10.0
-//   float32   1 x 4096 x 10240  63.1 / 71.1                  16 x 4096 x 10240 87.4 / 77.2
-//             1 x 1600 x 4288   13.7 / 16.2                  16 x 1600 x 4288  19.2 / 19.2
+// the call.  Few columns make work groups enough, more of them read x less often; the tiles
+// read x once for 32 and more.  us:
+//   bfloat16             8 columns  tiles     float32              8 columns  16 columns  tiles
+//    1 x 4096 x 10240        32       36       1 x 4096 x 10240        62         69       136
+//    8 x 4096 x 10240        37       38      16 x 4096 x 10240        89         79       137
+//   24 x 4096 x 10240        55       38       8 x 4096 x 4096         31         30        98
+//    2 x 1600 x 4288        8.4      9.1      32 x 4096 x 4096         54         41        99
+//    8 x 1600 x 4288        9.3      9.2      16 x 1600 x 4288         19         19        32
+//   24 x 1600 x 4288       13.2      9.2      32 x 8192 x 1024         46         65       164
+//   32 x 8192 x 1024         23       26
+//    8 x 5120 x 13824        66       54
 constexpr int kGatedRows = 32;
 inline int gated_rows_columns(int T, int F, bool bf16) {
   if (T > kGatedRows) return 0;
-  if (!bf16) return T > 4 && F >= 8192 ? 16 : 8;
-  if (F >= 8192) return T > 4 ? 0 : 8;
-  return T > 8 && F >= 4096 ? 32 : 8;
+  if (!bf16) return T > 8 && F >= 4096 ? 16 : 8;
+  if (T > 8) return F < 2048 ? 8 : 0;
+  return T > 4 && F >= 8192 ? 0 : 8;
 }
 
 // Floats of partial sums that a backward's products leave (one after the other, in one place).

@@ -54,7 +54,7 @@ def forms_of(case, p):
     return {fwd, (dtype, "dx", NAMES[xf], xp > 1), (dtype, "dw", NAMES[wf], wp > 1)}
 
 
-EVERY = {(d, "rows", n, many) for d, n in (("bf16", 8), ("bf16", 32), ("f32", 8), ("f32", 16)) for many in (False, True)} \
+EVERY = {(d, "rows", n, many) for d, n in (("bf16", 8), ("f32", 8), ("f32", 16)) for many in (False, True)} \
     | {("bf16", "fwd", n, False) for n in BF16 + ["128x64"]} | {("f32", "fwd", n, False) for n in F32} \
     | {("bf16", p, n, parts) for p in ("dx", "dw") for n in BF16 for parts in (False, True)} \
     | {("f32", p, n, parts) for p in ("dx", "dw") for n in F32 for parts in (False, True)}
