@@ -131,7 +131,7 @@ void ffn_tile_kernel(TileArgs<T> g) {
   if (n_mine <= 0) return;  // uniform over the group
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wk = w / (WP * WQ), wp = w % (WP * WQ) / WQ, wq = w % WQ;
+  const int wk = WK == 1 ? 0 : w / (WP * WQ), wp = (WK == 1 ? w : w % (WP * WQ)) / WQ, wq = w % WQ;
 
   // The items, 64 at a time, one per lane (the divisions run once for all of them).
   struct Item {
