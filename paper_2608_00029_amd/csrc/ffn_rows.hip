@@ -2,8 +2,8 @@
 //
 // The weights' bytes bound it: each is read once, straight into the operand
 // registers of the matrix cores, while x stays in the caches.  A work group takes
-// RF columns of h; its eight waves take the 128-byte lines of k in turn and keep a
-// step's loads in flight while the step before is contracted; their partial sums
+// RF columns of h; its eight waves take the 128-byte lines of k in turn and keep the
+// loads of the next steps in flight while one is contracted; their partial sums
 // meet in LDS, and the activation and the product are formed there.
 //
 // Matrix instructions are 16 x 16: rows are weights (8 gate and 8 up rows in one
@@ -94,18 +94,24 @@ __global__ __launch_bounds__(64 * kWaves) void ffn_rows_kernel(const T* __restri
 #pragma unroll
         for (int n = 0; n < NX; ++n) acc[i][n] = Pc::contract(s.a[i][j], s.b[n][j], acc[i][n]);
   };
-  constexpr int STRIDE = KS * kWaves;
-  Step s0, s1;
+  // Steps held, the loads of all but one on their way: as many as the registers of a block of
+  // tokens leave room for at four work groups a compute unit.  (2 / 3 / 4, us: bfloat16 1 x 4096 x
+  // 10240 32.5 / 31.2 / 29.5, 1 x 4096 x 4096 12.5 / 12.2 / 11.6; float32 1 x 2048 x 5632 21.9 / 20.4 /
+  // 20.3, 8 x 4096 x 10240 72.1 / 70.0 / 71.4; 1 x 1600 x 4288 8.0 in all.)
+  constexpr int STRIDE = KS * kWaves, DEPTH = RF > 8 || NX > 1 ? 2 : sizeof(T) == 2 ? 4 : 3;
+  Step st[DEPTH];
   int k = w * KS;
-  if (k < C) load(s0, k);
+#pragma unroll
+  for (int d = 0; d < DEPTH - 1; ++d)
+    if (k + d * STRIDE < C) load(st[d], k + d * STRIDE);
   while (k < C) {
-    if (k + STRIDE < C) load(s1, k + STRIDE);
-    contract(s0);
-    k += STRIDE;
-    if (k >= C) break;
-    if (k + STRIDE < C) load(s0, k + STRIDE);
-    contract(s1);
-    k += STRIDE;
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      if (k + (DEPTH - 1) * STRIDE < C) load(st[(d + DEPTH - 1) % DEPTH], k + (DEPTH - 1) * STRIDE);
+      contract(st[d]);
+      k += STRIDE;
+      if (k >= C) break;
+    }
   }
 
   // acc[i][n][j]: weight row 4 g + j of block i, token 16 n + m

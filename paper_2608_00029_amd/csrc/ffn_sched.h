@@ -80,7 +80,7 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
 // the call.  Few columns make work groups enough, more of them read x less often; the tiles
 // read x once for 32 and more.  us:
 //   bfloat16             8 columns  tiles     float32              8 columns  16 columns  tiles
-//    1 x 4096 x 10240        32       36       1 x 4096 x 10240        62         69       136
+//    1 x 4096 x 10240        30       36       1 x 4096 x 10240        62         69       136
 //    8 x 4096 x 10240        37       38      16 x 4096 x 10240        89         79       137
 //   24 x 4096 x 10240        55       38       8 x 4096 x 4096         31         30        98
 //    2 x 1600 x 4288        8.4      9.1      32 x 4096 x 4096         54         41        99
