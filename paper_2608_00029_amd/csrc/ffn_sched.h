@@ -8,8 +8,9 @@ namespace cattn {
 
 enum { FWD, DX, DW };
 
-// A form: a tile of p x q, and what it costs, in us, measured: a work group's chunk of
-// 128 bytes of k with every compute unit at work, and a tile's start and end.
+// A form: a tile of p x q, and what it costs, in units of 10 ns, measured: a work group's
+// chunk of 128 bytes of k with every compute unit at work, and a tile's start and end.
+// (Whole numbers: the workspace's size and the launch have to come to the same plan.)
 //
 // Large tiles pay least for their operands' way through L2 and LDS (a compute unit takes
 // about 60 bytes a ns), smaller ones leave fewer compute units idle in the last round and
@@ -29,13 +30,12 @@ enum { FWD, DX, DW };
 //             64 x 2048 x 5632        15.1       12.3     10.9
 //             39 x 3272 x 3568        24.4       17.1     15.7
 struct FfnForm {
-  int id, p, q;
-  float chunk, tile;
+  int id, p, q, chunk, tile;
 };
 enum { F256, F192, F256X128, F128, F64X128, F64, F128X64 };
-constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 1.30f, 3.f},
-                                {F256X128, 256, 128, 0.94f, 3.f}, {F128, 128, 128, 0.56f, 2.5f},
-                                {F128X64, 128, 64, 0.31f, 2.9f},  {F64, 64, 64, 0.27f, 2.5f}};
+constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 171, 400},    {F192, 192, 256, 130, 300},
+                                {F256X128, 256, 128, 94, 300}, {F128, 128, 128, 56, 250},
+                                {F128X64, 128, 64, 31, 290},   {F64, 64, 64, 27, 250}};
 // float32: the matrix cores' rate bounds all forms, and a compute unit's work groups share
 // it.  us:                    128 x 128  64 x 128  64 x 64
 //   dW  2048 x 768 x 2048         127       130      106
@@ -43,7 +43,7 @@ constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 1.71f, 4.f}, {F192, 192, 256, 1
 //   dW  4096 x 1024 x 2728        492       375      418
 //   forward  100 x 2048 x 4096              71       42
 //            300 x 1024 x 2048              38       39
-constexpr FfnForm kFfnF32[] = {{F128, 128, 128, 1.98f, 4.f}, {F64X128, 64, 128, 1.03f, 2.5f}, {F64, 64, 64, 0.53f, 2.f}};
+constexpr FfnForm kFfnF32[] = {{F128, 128, 128, 198, 400}, {F64X128, 64, 128, 103, 250}, {F64, 64, 64, 53, 200}};
 constexpr int kFfnUnits = 256;  // compute units
 
 struct FfnPlan {
@@ -55,7 +55,7 @@ struct FfnPlan {
 inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
   const int64_t chunk = bf16 ? 64 : 32, n = (K + chunk - 1) / chunk * (mode == DX ? 2 : 1);
   FfnPlan best{0, 1};
-  float best_us = 1e30f;
+  int64_t least = INT64_MAX;
   const FfnForm* forms = bf16 ? kFfnBf16 : kFfnF32;
   for (int i = 0; i < (bf16 ? 6 : 3); ++i) {
     const FfnForm& f = forms[i];
@@ -64,11 +64,11 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
     const int64_t tiles = ((M + f.p - 1) / f.p) * ((N + q - 1) / q) * (mode == DW ? 2 : 1);
     for (int parts = 1; parts <= (mode == FWD ? 1 : 32) && n >= 4 * (parts - 1); parts *= 2) {
       const int64_t rounds = (tiles * parts + kFfnUnits - 1) / kFfnUnits, each = (n + parts - 1) / parts;
-      float us = (float)rounds * ((float)each * f.chunk + f.tile);
+      int64_t cost = rounds * (each * f.chunk + f.tile);
       // parts: another kernel, and their floats out and in at 4 TB/s
-      if (parts > 1) us += 6.f + 2e-6f * (float)(parts * M * N * (mode == DW ? 2 : 1));
-      if (us < best_us) {
-        best_us = us;
+      if (parts > 1) cost += 600 + parts * M * N * (mode == DW ? 2 : 1) / 5000;
+      if (cost < least) {
+        least = cost;
         best = FfnPlan{f.id, parts};
       }
     }
