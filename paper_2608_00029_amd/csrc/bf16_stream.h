@@ -138,10 +138,12 @@ __device__ __forceinline__ unsigned lds_addr(const char* p) {
 // tile_barrier) before the barrier that publishes a tile.
 // M0 is a reserved register to the compiler, which warns about the clobber;
 // the clobber is what keeps it from assuming M0 survives the statement.
+// The s_nop is the wait state that the copy needs behind a scalar write of M0,
+// which neither the hardware nor, inside the statement, the compiler inserts.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void dma16(const void* sbase, unsigned voff, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(sbase)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(sbase)
                : "memory", "m0");
 }
 #pragma clang diagnostic pop

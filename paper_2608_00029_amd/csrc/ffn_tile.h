@@ -66,7 +66,7 @@ template <> struct Step<float> {
 #pragma clang diagnostic ignored "-Winline-asm"
 // One 16-byte HBM -> LDS copy per lane, from a per-lane address (see dma16).
 __device__ __forceinline__ void copy16(const void* src, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 

@@ -60,7 +60,8 @@ constexpr float kSumMax = 4294967296.0f;  // bound of a block's probability sum 
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 template <int OFF> __device__ __forceinline__ void dma16_at(const void* sbase, unsigned voff, unsigned lds) {
-  asm volatile("s_add_u32 m0, %0, %3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(sbase), "i"(OFF)
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(sbase),
+               "i"(OFF)
                : "memory", "m0", "scc");
 }
 #pragma clang diagnostic pop
