@@ -59,8 +59,15 @@ def gated_fwd(x, w_gate, w_up, activation: str = "silu", save: bool = False):
     return h, gate, up
 
 
+class _UnsupportedType(TypeError, KeyError):  # (a KeyError too: callers may catch it as one)
+    __str__ = Exception.__str__
+
+
 @functools.lru_cache(maxsize=256)
 def gated_bwd_workspace_bytes(T: int, C: int, F: int, dtype: torch.dtype = torch.float32) -> int:
+    """Bytes of gated_bwd's workspace; 0 for sizes that it refuses."""
+    if dtype not in _CODES:
+        raise _UnsupportedType(f"unsupported dtype {dtype}: use float32 or bfloat16")
     return int(lib().cattn_gated_bwd_workspace_bytes(_int(T), _int(C), _int(F), _CODES[dtype]))
 
 
