@@ -95,8 +95,8 @@ __global__ __launch_bounds__(64 * kWaves) void ffn_rows_kernel(const T* __restri
         for (int n = 0; n < NX; ++n) acc[i][n] = Pc::contract(s.a[i][j], s.b[n][j], acc[i][n]);
   };
   // Steps held, the loads of all but one on their way.  (2 / 3 / 4, us: bfloat16 1 x 4096 x 10240
-  // 32.5 / 31.2 / 29.5, 1 x 4096 x 4096 12.5 / 12.2 / 11.6, 1 x 1600 x 4288 8.0 in all; float32 1 x 2048 x
-  // 5632 21.9 / 20.4 / 20.3, 8 x 4096 x 10240 72.1 / 70.0 / 71.4.)
+  // 31.0 / 29.7 / 28.7, 1 x 4096 x 4096 15.4 / 13.5 / 12.7, 1 x 1600 x 4288 7.8 / 7.8 / 8.2; float32 1 x
+  // 2048 x 5632 19.4 / 18.1 / 18.3, 8 x 4096 x 10240 67.6 / 67.3 / 67.1.)
   constexpr int STRIDE = KS * kWaves, DEPTH = RF > 8 || NX > 1 ? 2 : sizeof(T) == 2 ? 4 : 3;
   Step st[DEPTH];
   int k = w * KS;

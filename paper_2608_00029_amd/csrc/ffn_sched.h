@@ -8,27 +8,38 @@ namespace cattn {
 
 enum { FWD, DX, DW };
 
-// A form: a tile of p x q, and what it costs, in units of 10 ns, measured: a work group's
-// chunk of 128 bytes of k with every compute unit at work, and a tile's start and end.
-// (Whole numbers: the workspace's size and the launch have to come to the same plan.)
+// A form: a tile of p x q, and what it costs, in units of 10 ns, fitted to measurements: a
+// work group's chunk of 128 bytes of k with every compute unit at work, and a tile's start
+// and end.  (Whole numbers: the workspace's size and the launch have to come to the same plan.)
+// Where few units work a chunk takes less, where HBM holds the operands of few tiles more: the
+// chosen forms' times by them come out a third below to a fifth above those that follow.  It
+// is their order that counts: over 30 drawn shapes in bfloat16 the plan took 1.02 - 1.03 times
+// the best of all forms and parts (geometric mean of each product), a single one up to 1.29;
+// over 15 in float32 1.03, dx 1.09, dW 1.01, a single one up to 1.39.
 //
-// Large tiles pay least for their operands' way through L2 and LDS (a compute unit takes
-// about 60 bytes a ns), smaller ones leave fewer compute units idle in the last round and
-// at the edges.  bfloat16, us:             256 x 256  192 x 256  256 x 128  128 x 128
-//   forward  4096 x 4096 x 10240               572        592        630        758
-//            3777 x 1024 x 2728                 59         52         58         71
-//            1024 x 1024 x 2728                 29         26         21         23
-//   dW       3777 x 1024 x 2728                 80         66         56         69
-//   dx       3777 x 1024 x 2728                107         85         75         57
-// The smallest has four chunks ahead in place of two, which is what few work groups need to
-// keep HBM busy (24 x 4096 x 10240: 38.6 us, with two ahead 53.9), and reads fragments three
-// steps ahead (200 x 2048 x 5632: 18.8, one step 21.2; 256 x 128 loses by it, 630 to 738).
-// Fewer tiles yet than compute units: a chunk's k-steps are shared by two sets of waves.
+// us, in one run, whole k, operands from HBM.  Large tiles pay least for their operands'
+// way through L2 and LDS (a compute unit takes about 60 bytes a ns), smaller ones leave fewer
+// compute units idle in the last round and at the edges.
+//   bfloat16                     256 x 256  192 x 256  256 x 128  128 x 128
+//   forward  4096 x 4096 x 10240       521        561        589        715
+//            8192 x 1600 x 4288        197        196        209        238
+//              with gate and up        212        218        248        283
+//            3777 x 1024 x 2728         50         45         48         55
+//            1024 x 1024 x 2728         24         21         17         20
+//   dW       8192 x 1600 x 4288        194        258        213        254
+//            3777 x 1024 x 2728         73         59         49         61
+//   dx       8192 x 1600 x 4288        192        264        210        263
+//            3777 x 1024 x 2728         96         76         66         52
+// 128 x 128 has four chunks ahead in place of two, which is what few work groups need to keep
+// HBM busy (24 x 4096 x 10240: 39 us, with two ahead 56; 200 x 2048 x 5632: 20 and 29), and reads
+// fragments three steps ahead (here as fast as one; 256 x 128 loses by it, 598 to 694).
+// Fewer tiles yet than compute units: in 128 x 64 and 64 x 64 (three and four chunks ahead,
+// fragments one step) a chunk's k-steps are shared by two sets of waves.
 //                                  128 x 128  128 x 64  64 x 64
-//   forward  200 x 2048 x 5632        17.2       22.2     25.5
-//            100 x 2048 x 5632        15.7       12.8     17.7
-//             64 x 2048 x 5632        15.1       12.3     10.9
-//             39 x 3272 x 3568        24.4       17.1     15.7
+//   forward  200 x 2048 x 5632            20        28       28
+//            100 x 2048 x 5632            20        17       21
+//             64 x 2048 x 5632            18        16       13
+//             39 x 3272 x 3568            37        24       23
 struct FfnForm {
   int id, p, q, chunk, tile;
 };
@@ -38,11 +49,11 @@ constexpr FfnForm kFfnBf16[] = {{F256, 256, 256, 171, 400},    {F192, 192, 256, 
                                 {F128X64, 128, 64, 31, 290},   {F64, 64, 64, 27, 250}};
 // float32: the matrix cores' rate bounds all forms, and a compute unit's work groups share
 // it.  us:                    128 x 128  64 x 128  64 x 64
-//   dW  2048 x 768 x 2048         127       130      106
-//   dx  4096 x 1024 x 2728        342       354      375
-//   dW  4096 x 1024 x 2728        492       375      418
-//   forward  100 x 2048 x 4096              71       42
-//            300 x 1024 x 2048              38       39
+//   dW  2048 x 768 x 2048         127       130      105
+//   dx  4096 x 1024 x 2728        339       349      365
+//   dW  4096 x 1024 x 2728        500       375      411
+//   forward  100 x 2048 x 4096    130        72       54
+//            300 x 1024 x 2048     68        38       38
 constexpr FfnForm kFfnF32[] = {{F128, 128, 128, 198, 400}, {F64X128, 64, 128, 103, 250}, {F64, 64, 64, 53, 200}};
 constexpr int kFfnUnits = 256;  // compute units
 
@@ -78,16 +89,21 @@ inline FfnPlan ffn_plan(int mode, int64_t M, int64_t N, int64_t K, bool bf16) {
 
 // Columns of h that a work group of the forward's few-rows kernel takes; 0: the tiles take
 // the call.  Few columns make work groups enough, more of them read x less often; the tiles
-// read x once for 32 and more.  us:
+// read x once for 32 and more.  us, in one run, operands from HBM:
 //   bfloat16             8 columns  tiles     float32              8 columns  16 columns  tiles
-//    1 x 4096 x 10240        30       36       1 x 4096 x 10240        62         69       136
-//    8 x 4096 x 10240        37       38      16 x 4096 x 10240        89         79       137
-//   24 x 4096 x 10240        55       38       8 x 4096 x 4096         31         30        98
-//    2 x 1600 x 4288        8.4      9.1      32 x 4096 x 4096         54         41        99
-//    8 x 1600 x 4288        9.3      9.2      16 x 1600 x 4288         19         19        32
-//   24 x 1600 x 4288       13.2      9.2      32 x 8192 x 1024         46         65       164
+//    1 x 4096 x 10240        29       37       1 x 4096 x 10240        58         67       137
+//    4 x 4096 x 10240        30       39       8 x 4096 x 4096         29         29        98
+//    6 x 4096 x 10240        32       39      16 x 4096 x 10240        86         80       138
+//    8 x 4096 x 10240        35       37      32 x 4096 x 4096         53         40       102
+//    5 x 5120 x 13824        55       53      16 x 1600 x 4288         22         22        41
+//    8 x 5120 x 13824        61       52      32 x 8192 x 1024         50         68       185
+//    2 x 1600 x 4288        8.5      8.6
+//    8 x 1600 x 4288        9.1      8.6
+//   24 x 1600 x 4288       13.1      8.7
+//   24 x 4096 x 10240        55       37
 //   32 x 8192 x 1024         23       26
-//    8 x 5120 x 13824        66       54
+// (5 to 8 tokens of 8192 columns and more: the tiles, which lose up to 6 us at 4096 x 10240 and
+// gain up to 9 at 5120 x 13824.)
 constexpr int kGatedRows = 32;
 inline int gated_rows_columns(int T, int F, bool bf16) {
   if (T > kGatedRows) return 0;

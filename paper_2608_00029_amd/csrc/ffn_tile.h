@@ -18,13 +18,13 @@
 // what is in flight on it fits its L2.  Ends: rows past the end are read from the last one
 // and not stored; pieces of a chunk past the end of k come from a line of zeros.
 //
-// Rates reached, bfloat16, 256 x 256 tiles: 4096 x 4096 x 10240 522 us forward (1317
-// TFLOP/s), 504 dx, 527 dW, where the matrix cores are busy 72% of the cycles and the clock
-// is down to 1.5 - 1.9 GHz by power.  Found on the way there (forward, that size, us): chunks
-// of 64 bytes, half lines, 587, whole lines 527; fragments asked for before a k-step's first
-// contraction 587, after it 566; the same work without any copy 466, without the barrier too
-// 461; every line in L2 530 where 567 were then measured; four waves of 96 x 128 619 where
-// eight took 592.
+// Rates reached, bfloat16, 256 x 256 tiles: 4096 x 4096 x 10240 521 us forward (1319
+// TFLOP/s), 515 dx, 540 dW, where the matrix cores are busy 72% of the cycles and the clock
+// is down to 1.5 - 1.9 GHz by power.  Found on the way there (forward, that size, us, each
+// beside the kernel of its time): chunks of 64 bytes, half lines, 587, whole lines 527;
+// fragments asked for before a k-step's first contraction 587, after it 566; the same work
+// without any copy 466, without the barrier too 461; every line in L2 530 where 567 were then
+// measured; four waves of 96 x 128 619 where eight took 592.
 #pragma once
 
 #include <algorithm>
@@ -37,8 +37,8 @@
 namespace cattn {
 
 // Row tiles that a chiplet takes side by side.  (4 / 6 / 8 / 16, us: forward 4096 x 4096 x
-// 10240 522 / 532 / 533 / 540, 8192 x 1600 x 4288 218 / 217 / 221 / 229, dW of 2048 x 2048 x
-// 5632 104 / 104 / 107 / 108.)
+// 10240 522 / 517 / 521 / 525, 8192 x 1600 x 4288 196 / 197 / 196 / 198, dW of 2048 x 2048 x
+// 5632 87 / 88 / 87 / 88: it matters little.)
 constexpr int kGroup = 4;
 
 static __device__ __attribute__((aligned(16))) const unsigned kZeros[4] = {0, 0, 0, 0};

@@ -44,7 +44,8 @@ def _gated_inputs(where, x, w_gate, w_up, activation):
 def gated_fwd(x, w_gate, w_up, activation: str = "silu", save: bool = False):
     """(h, gate, up): h = act(x w_gate^T) * (x w_up^T) over the last axis of x.
 
-    x [..., C]; w_gate, w_up [F, C]; h [..., F]; float32 or bfloat16, contiguous.
+    x [..., C]; w_gate, w_up [F, C]; h [..., F]; float32 or bfloat16, contiguous, from
+    a 16-byte boundary on; C and F multiples of 8.
     activation: "silu", or "gelu" (the tanh form).  save: the two products are kept
     for gated_bwd; without it gate and up are None.
     """
@@ -72,7 +73,7 @@ def gated_bwd_workspace_bytes(T: int, C: int, F: int, dtype: torch.dtype = torch
 
 
 def gated_bwd(x, w_gate, w_up, gate, up, dh, activation: str = "silu", workspace=None):
-    """(dx, dw_gate, dw_up) of gated_fwd for upstream dh, given its gate and up."""
+    """(dx, dw_gate, dw_up) of gated_fwd for upstream dh, given its gate and up; tensors as there."""
     T, C, F, act, code = _gated_inputs("cattn_gated_bwd", x, w_gate, w_up, activation)
     shape = x.shape[:-1] + (F,)
     for name, t in (("gate", gate), ("up", up), ("dh", dh)):
@@ -108,7 +109,8 @@ def _dropout_numbers(seed, site, step, device):
 def dropout_fwd(x, p: float, seed: int, site: int = 0, step=0, residual=None, y=None):
     """y = residual + x / (1 - p) where kept, residual (or 0) elsewhere; no mask is stored.
 
-    x (and residual, y): float32 or bfloat16, contiguous, any shape.  An element's
+    x (and residual, y): float32 or bfloat16, contiguous, any shape, from a 16-byte
+    boundary on (a slice such as x[1:] may begin elsewhere: clone it).  An element's
     fate depends on seed, site, step and its index alone: dropout_bwd with the same
     ones drops the same.  site: which of the model's dropouts this is; step: an
     integer, or an int64 tensor [1] on x's device, which is read when the kernel
